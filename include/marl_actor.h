@@ -374,6 +374,99 @@ int marl_selftest_bounded_wait(void* stream, uint32_t poll_limit, uint32_t* stat
  * at the clocks it actually sustains.  SYNCHRONISES the stream; takes a few tens of milliseconds. */
 int marl_measure_ffma_tflops(void* stream, double* tflops_out);
 
+/* ---- The learner's side -------------------------------------------------------------------------------------------
+ * What stands between marl_ring_sample and marl_actor_publish_weights (Algorithm 3: the learner draws a batch, computes the
+ * gradient of its loss and updates the model; the paper prints none of the operators, so their definitions are this
+ * library's).  These functions need no actor.  All arrays are DEVICE memory of the device that is current, owned by the caller;
+ * the work is enqueued on `stream` (a cudaStream_t of that device, NULL = the legacy default stream), asynchronous, and may be
+ * captured into a graph.  Nothing is allocated and nothing is kept between calls; outputs must not overlap inputs unless a
+ * function says so. */
+#define MARL_DTYPE_FP32 0
+#define MARL_DTYPE_BF16 1
+#define MARL_DTYPE_FP16 2
+
+#define MARL_MAX_TOP 32
+
+/* Rows of action values (the q of a sampled batch: rows = B * ring_steps * n_agents). */
+typedef struct {
+  const void* logits;     /* [rows][n_actions] of dtype; row r starts row_stride elements after row r - 1 */
+  const uint8_t* avail;   /* [rows][n_actions], non-zero = available, rows avail_stride bytes apart; NULL: all available */
+  const int32_t* action;  /* [rows] the action taken; outside [0, n_actions): none */
+  int64_t rows;           /* >= 0 */
+  int64_t row_stride;     /* >= 0; 0: the same row every time */
+  int64_t avail_stride;   /* >= 0; 0: the same availability for every row */
+  int32_t n_actions;      /* 1 .. 2^30 */
+  int32_t dtype;          /* MARL_DTYPE_*: of logits and of their gradient */
+  float temperature;      /* > 0, finite */
+  int32_t reserved;       /* 0 */
+} marl_policy_rows_t;
+
+/* The Boltzmann policy p_j = exp(x_j / temperature) / sum over the available entries, of each row x.  An entry whose value is
+ * -infinity counts as unavailable; the value of an unavailable entry, a NaN included, has no effect.
+ *   logp f32[rows]       log p of the action taken; -infinity if that action is unavailable; 0 for a row without an action and
+ *                        for an empty row (no available entry: a step behind the end of a sampled episode)
+ *   entropy f32[rows]    -sum p log p; 0 for an empty row
+ *   stats f32[rows][2]   the largest available value and the logarithm of sum exp((x_j - largest) / temperature): what
+ *                        the gradient needs of the row; -infinity, -infinity for an empty row
+ *   top_index i32[rows][top], top_logp f32[rows][top]: the `top` (0 .. MARL_MAX_TOP) most probable available actions,
+ *                        descending, the lower index first among equal values, and their log probabilities; -1 and -infinity where
+ *                        there are fewer.  NULL with top = 0.
+ * A row with a NaN or +infinity among its available entries has NaN results (a NaN ranks above all numbers among the
+ * alternatives).  Sums are held in fp32, relative to the running maximum. */
+int marl_policy_logprob(void* stream, const marl_policy_rows_t* in, int32_t top, float* logp, float* entropy, float* stats,
+                        int32_t* top_index, float* top_logp);
+
+/* The gradient of marl_policy_logprob with respect to the logits, from the stats and the entropy that it wrote:
+ *   dlogits_j = 1/temperature * (g_logp (1[j = action] - p_j) - g_entropy p_j (log p_j + entropy))
+ * for available entries, 0 for the others, for empty rows, and (its first term) for rows without an action.  g_logp and
+ * g_entropy f32[rows], either may be NULL (no gradient from there).  dlogits [rows][n_actions] of in->dtype, rows dlogits_stride (>= n_actions) elements
+ * apart, is written in full; what lies between its rows is left as it is.  It may be the logits themselves (same address and row
+ * distance).  The alternatives have no gradient. */
+int marl_policy_logprob_backward(void* stream, const marl_policy_rows_t* in, const float* stats, const float* entropy,
+                                 const float* g_logp, const float* g_entropy, void* dlogits, int64_t dlogits_stride);
+
+/* The gated linear recurrence over a batch of episodes: per sequence b and channel c, step by step in scan order,
+ *   MARL_SCAN_RAW:    h' = gate * h + x
+ *   MARL_SCAN_BLEND:  h' = (1 - z) * x + z * h,  z = 1 / (1 + exp(-gate))      (the blend of the agent's GRU cell)
+ * and y = h'.  Forwards the scan order is t = 0, 1, ..., length[b] - 1, in reverse it is t = length[b] - 1, ..., 0 (discounted
+ * returns: gate = discount, x = reward, h0 = bootstrap value).  done[b][t] cuts between step t and step t + 1, as the ring
+ * records it: no state passes from either to the other, whatever its value.  h0 enters the first step of the scan order (in reverse
+ * it is dropped if done[b][length[b] - 1] is set: the game had ended).  `last` is the state that passes on behind the last step: in
+ * reverse y[b][0], forwards y[b][length[b] - 1], or 0 if done is set there; h0 for a sequence of length 0.  So a run over the
+ * steps [0, s) and one over [s, L) with its `last` as h0 give what one run over [0, L) gives.
+ * The state is held in fp32.  It is computed from products of neighbouring gates: raw gates are meant to be of modulus up to about 1,
+ * and products of a few hundred of them that overflow fp32 give infinities or NaN; an infinite or NaN state stays on this side of a cut and
+ * of its sequence and channel. */
+#define MARL_SCAN_RAW 0
+#define MARL_SCAN_BLEND 1
+#define MARL_SCAN_INTERVAL 64 /* steps between two kept states */
+typedef struct {
+  const void* gate;       /* element (b, t, c) at gate[b * gate_b + t * gate_t + c * gate_c], of dtype; strides >= 0 in elements */
+  const void* x;          /* likewise */
+  int64_t gate_b, gate_t, x_b, x_t;
+  int32_t gate_c, x_c;    /* 0 (one value for all channels) or 1 */
+  const float* h0;        /* [B][C]; NULL: 0 */
+  const uint8_t* done;    /* [B][L]; NULL: none */
+  const int32_t* length;  /* [B], taken as at least 0 and at most L; NULL: L */
+  int32_t B, L, C;        /* >= 0 */
+  int32_t dtype, form, reverse;
+} marl_scan_t;
+
+/* Bytes that a call needs: states (for the gradient) and work (both directions; 0 for most sizes). */
+int marl_linear_scan_query(const marl_scan_t* in, size_t* states_bytes, size_t* work_bytes);
+
+/* y [B][L][C] of dtype: 0 at and behind the end of a sequence, where the inputs are not read.  last f32[B][C].  states
+ * f32[B][ceil(L / MARL_SCAN_INTERVAL)][C], the state that enters every MARL_SCAN_INTERVAL-th step in scan order, for the gradient (those
+ * behind a sequence's end are not written); NULL: not kept.  work: scratch of at least work_bytes as queried, 8-byte aligned, may be
+ * NULL if that is 0. */
+int marl_linear_scan(void* stream, const marl_scan_t* in, void* y, float* last, float* states, void* work, size_t work_bytes);
+
+/* The gradients, given those of y (dy, of dtype, element (b, t, c) at dy[b * dy_b + t * dy_t + c]) and of last (dlast f32[B][C],
+ * NULL: 0).  dgate, dx [B][L][C] of dtype, dense also where gate or x were broadcast (the caller sums), 0 behind a sequence's end;
+ * dh0 f32[B][C], may be NULL.  The states between the kept ones are computed again, in fp32, from gate and x. */
+int marl_linear_scan_backward(void* stream, const marl_scan_t* in, const float* states, const void* dy, int64_t dy_b, int64_t dy_t,
+                              const float* dlast, void* dgate, void* dx, float* dh0, void* work, size_t work_bytes);
+
 /* Name of the step kernel in use: "ffma" (the general path: split-operand tensor-core or CUDA-core kernel), "tcgen05"
  * (one-tile tensor-core kernel), "tcgen05-pipelined", "tcgen05-dual" (two resident tiles; its other launches run on the pipelined kernel), or
  * "tcgen05-streamed" (hidden size 128: weights kept in shared memory as far as they fit, the others streamed). */

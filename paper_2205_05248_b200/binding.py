@@ -36,8 +36,13 @@ EXPORTS = [
     "marl_actor_status", "marl_actor_reset", "marl_actor_destroy", "marl_actor_kernel_name",
     "marl_actor_step_kernel",
     "marl_actor_launch_count", "marl_last_error", "marl_rollout_noalloc", "marl_selftest_bounded_wait",
-    "marl_measure_ffma_tflops",
+    "marl_measure_ffma_tflops", "marl_policy_logprob", "marl_policy_logprob_backward",
+    "marl_linear_scan_query", "marl_linear_scan", "marl_linear_scan_backward",
 ]
+DTYPE = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+MAX_TOP = 32
+SCAN_FORM = {"raw": 0, "blend": 1}
+SCAN_INTERVAL = 64
 
 
 class MarlError(RuntimeError):
@@ -80,6 +85,19 @@ class RingView(C.Structure):
 class StateView(C.Structure):
     _fields_ = [("h", C.c_void_p), ("last_action", C.c_void_p), ("slot", C.c_void_p), ("pos", C.c_void_p),
                 ("ep_count", C.c_void_p), ("step", C.c_uint64)]
+
+
+class PolicyRows(C.Structure):
+    _fields_ = [("logits", C.c_void_p), ("avail", C.c_void_p), ("action", C.c_void_p), ("rows", C.c_int64),
+                ("row_stride", C.c_int64), ("avail_stride", C.c_int64), ("n_actions", C.c_int32), ("dtype", C.c_int32),
+                ("temperature", C.c_float), ("reserved", C.c_int32)]
+
+
+class Scan(C.Structure):
+    _fields_ = [("gate", C.c_void_p), ("x", C.c_void_p), ("gate_b", C.c_int64), ("gate_t", C.c_int64), ("x_b", C.c_int64),
+                ("x_t", C.c_int64), ("gate_c", C.c_int32), ("x_c", C.c_int32), ("h0", C.c_void_p), ("done", C.c_void_p),
+                ("length", C.c_void_p), ("B", C.c_int32), ("L", C.c_int32), ("C", C.c_int32), ("dtype", C.c_int32),
+                ("form", C.c_int32), ("reverse", C.c_int32)]
 
 
 class Counters(C.Structure):
@@ -132,6 +150,11 @@ def load_library():
         lib.marl_actor_set_state.argtypes = [P, C.POINTER(StateView)]
         lib.marl_actor_status.argtypes = [P, C.POINTER(C.c_uint32), C.POINTER(Counters)]
         lib.marl_actor_reset.argtypes = [P]
+        lib.marl_policy_logprob.argtypes = [P, C.POINTER(PolicyRows), C.c_int32, P, P, P, P, P]
+        lib.marl_policy_logprob_backward.argtypes = [P, C.POINTER(PolicyRows), P, P, P, P, P, C.c_int64]
+        lib.marl_linear_scan_query.argtypes = [C.POINTER(Scan), C.POINTER(C.c_size_t), C.POINTER(C.c_size_t)]
+        lib.marl_linear_scan.argtypes = [P, C.POINTER(Scan), P, P, P, P, C.c_size_t]
+        lib.marl_linear_scan_backward.argtypes = [P, C.POINTER(Scan), P, P, C.c_int64, C.c_int64, P, P, P, P, P, C.c_size_t]
         _lib = lib
     return _lib
 
@@ -183,6 +206,172 @@ def marl_selftest_bounded_wait(poll_limit: int = 20000) -> int:
 
 def _dptr(t):
     return None if t is None else C.c_void_p(t.data_ptr())
+
+
+# ---- the learner's operators (device tensors, on the current stream of their device) ------------------------------------
+def _need(ok: bool, text: str):
+    if not ok:
+        raise MarlError(text)
+
+
+def _device_call(dev, fn, *args):
+    """fn(stream, *args) with the tensors' device current, on its current stream."""
+    stream = C.c_void_p(torch.cuda.current_stream(dev).cuda_stream)
+    if torch.cuda.current_device() == dev.index:
+        _check(fn(stream, *args))
+    else:
+        with torch.cuda.device(dev):
+            _check(fn(stream, *args))
+
+
+def _same_device(dev, **tensors):
+    for name, t in tensors.items():
+        _need(t is None or t.device == dev, f"{name} is not on {dev}")
+
+
+def _rows_of(t, name: str):
+    """t[..., A] as rows: (number of rows, elements between rows); the elements of a row must be neighbours."""
+    A = t.shape[-1]
+    _need(A >= 1, f"{name} has no entries")
+    _need(t.stride(-1) == 1 or A == 1, f"the entries of a row of {name} are not neighbours")
+    if t.numel() == 0:
+        return 0, A
+    if t.dim() == 2:
+        return t.shape[0], (t.stride(0) if t.shape[0] > 1 else A)
+    rows, stride = 1, None
+    for n, s in zip(reversed(t.shape[:-1]), reversed(t.stride()[:-1])):
+        if n == 1:
+            continue
+        if stride is None:
+            stride = s
+        else:
+            _need(s == stride * rows, f"{name} cannot be walked as rows at one distance")
+        rows *= n
+    return rows, (A if stride is None else stride)
+
+
+def _dense(t, dtype, shape, name: str):
+    if t is None:
+        return None
+    _need(t.dtype == dtype, f"{name} must be {dtype}")
+    _need(tuple(t.shape) == tuple(shape), f"{name} must have shape {tuple(shape)}")
+    _need(t.is_contiguous(), f"{name} must be contiguous")
+    return t
+
+
+def _policy_rows(logits, action, avail, temperature: float):
+    _need(logits.is_cuda, "logits must be a CUDA tensor: there is no CPU path")
+    _need(logits.dtype in DTYPE, "logits must be float32, bfloat16 or float16")
+    _need(logits.dim() >= 1, "logits must have at least one dimension")
+    lead, A = tuple(logits.shape[:-1]), logits.shape[-1]
+    rows, stride = _rows_of(logits, "logits")
+    _same_device(logits.device, action=action, avail=avail)
+    _dense(action, torch.int32, lead, "action")
+    astride = 0
+    if avail is not None:
+        _need(avail.dtype in (torch.uint8, torch.bool) and tuple(avail.shape) == tuple(logits.shape),
+              "avail must be uint8 or bool of the logits' shape")
+        astride = _rows_of(avail, "avail")[1]
+    return lead, PolicyRows(_dptr(logits), _dptr(avail), _dptr(action), rows, stride, astride, A, DTYPE[logits.dtype],
+                            float(temperature), 0)
+
+
+def marl_policy_logprob(logits, action, avail=None, temperature: float = 1.0, top: int = 0) -> dict:
+    """Log probability of the action taken, entropy and the `top` best alternatives of each row of logits [..., A] (the q of a
+    sampled batch).  action int32 [...], avail uint8 or bool [..., A].  Returns logp, entropy float32 [...], stats float32
+    [..., 2] (for the gradient), top_index int32 and top_logp float32 [..., top] (None with top = 0)."""
+    lead, p = _policy_rows(logits, action, avail, temperature)
+    _need(0 <= top <= MAX_TOP, f"top must be in [0, {MAX_TOP}]")
+    f32 = dict(dtype=torch.float32, device=logits.device)
+    out = dict(logp=torch.empty(lead, **f32), entropy=torch.empty(lead, **f32), stats=torch.empty(lead + (2,), **f32),
+               top_index=None, top_logp=None)
+    if top:
+        out["top_index"] = torch.empty(lead + (top,), dtype=torch.int32, device=logits.device)
+        out["top_logp"] = torch.empty(lead + (top,), **f32)
+    _device_call(logits.device, load_library().marl_policy_logprob, C.byref(p), C.c_int32(top), _dptr(out["logp"]),
+                 _dptr(out["entropy"]), _dptr(out["stats"]), _dptr(out["top_index"]), _dptr(out["top_logp"]))
+    return out
+
+
+def marl_policy_logprob_backward(logits, action, stats, entropy, g_logp=None, g_entropy=None, avail=None,
+                                 temperature: float = 1.0, out=None):
+    """The gradient of marl_policy_logprob with respect to the logits, from its stats and entropy and the gradients of logp and
+    entropy float32 [...] (either may be None).  Returns a tensor like logits (dense, or `out`, whose rows may be further apart)."""
+    lead, p = _policy_rows(logits, action, avail, temperature)
+    _same_device(logits.device, stats=stats, entropy=entropy, g_logp=g_logp, g_entropy=g_entropy, out=out)
+    _dense(stats, torch.float32, lead + (2,), "stats")
+    for name, t in (("entropy", entropy), ("g_logp", g_logp), ("g_entropy", g_entropy)):
+        _dense(t, torch.float32, lead, name)
+    if out is None:
+        out = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
+    _need(out.dtype == logits.dtype and out.shape == logits.shape, "out must be like logits")
+    _device_call(logits.device, load_library().marl_policy_logprob_backward, C.byref(p), _dptr(stats), _dptr(entropy),
+                 _dptr(g_logp), _dptr(g_entropy), _dptr(out), C.c_int64(_rows_of(out, "out")[1]))
+    return out
+
+
+def _scan_args(gate, x, h0, done, length, form: str, reverse: bool):
+    _need(x.is_cuda, "x must be a CUDA tensor: there is no CPU path")
+    _need(x.dtype in DTYPE and gate.dtype == x.dtype, "gate and x must both be float32, bfloat16 or float16")
+    _need(x.dim() == 3 and gate.shape == x.shape, "gate and x must have the same shape [B, L, C]")
+    _need(form in SCAN_FORM, f"form must be one of {sorted(SCAN_FORM)}")
+    B, L, Cn = x.shape
+    _same_device(x.device, gate=gate, h0=h0, done=done, length=length)
+    _dense(h0, torch.float32, (B, Cn), "h0")
+    _dense(length, torch.int32, (B,), "length")
+    if done is not None:
+        _need(done.dtype in (torch.uint8, torch.bool), "done must be uint8 or bool")
+        _dense(done, done.dtype, (B, L), "done")
+    step = []
+    for name, t in (("gate", gate), ("x", x)):
+        c = t.stride(2) if Cn > 1 else 1
+        _need(c in (0, 1), f"the channels of {name} must be neighbours, or one value for all")
+        step.append((t.stride(0), t.stride(1), c))
+    (gb, gt, gc), (xb, xt, xc) = step
+    return Scan(_dptr(gate), _dptr(x), gb, gt, xb, xt, gc, xc, _dptr(h0), _dptr(done), _dptr(length), B, L, Cn, DTYPE[x.dtype],
+                SCAN_FORM[form], int(bool(reverse)))
+
+
+def _scan_work(s, dev):
+    need = C.c_size_t()
+    _check(load_library().marl_linear_scan_query(C.byref(s), None, C.byref(need)))
+    work = torch.empty(need.value, dtype=torch.uint8, device=dev) if need.value else None
+    return work, C.c_size_t(need.value)
+
+
+def marl_linear_scan(gate, x, h0=None, done=None, length=None, form: str = "blend", reverse: bool = False, keep: bool = False) -> dict:
+    """The gated linear recurrence of x [B, L, C] (its rows and those of gate may be strided; gate may be expanded).  h0 float32 [B, C],
+    done uint8 or bool [B, L], length int32 [B], each may be None.  Returns y like x (dense), last float32 [B, C] and, with
+    keep, the states that marl_linear_scan_backward takes."""
+    s = _scan_args(gate, x, h0, done, length, form, reverse)
+    B, L, Cn = x.shape
+    out = dict(y=torch.empty((B, L, Cn), dtype=x.dtype, device=x.device),
+               last=torch.empty((B, Cn), dtype=torch.float32, device=x.device), states=None)
+    if keep:
+        out["states"] = torch.empty((B, -(-L // SCAN_INTERVAL), Cn), dtype=torch.float32, device=x.device)
+    work, need = _scan_work(s, x.device)
+    _device_call(x.device, load_library().marl_linear_scan, C.byref(s), _dptr(out["y"]), _dptr(out["last"]), _dptr(out["states"]),
+                 _dptr(work), need)
+    return out
+
+
+def marl_linear_scan_backward(gate, x, states, dy, dlast=None, h0=None, done=None, length=None, form: str = "blend",
+                              reverse: bool = False) -> dict:
+    """The gradients of marl_linear_scan (called with the same arguments and keep=True) from those of y and, if not None, of last:
+    dgate and dx like x (dense; the caller sums them where the inputs were expanded) and dh0 float32 [B, C]."""
+    s = _scan_args(gate, x, h0, done, length, form, reverse)
+    B, L, Cn = x.shape
+    _same_device(x.device, states=states, dy=dy, dlast=dlast)
+    _dense(states, torch.float32, (B, -(-L // SCAN_INTERVAL), Cn), "states")
+    _dense(dlast, torch.float32, (B, Cn), "dlast")
+    _need(dy.dtype == x.dtype and dy.shape == x.shape, "dy must be like x")
+    _need(dy.stride(2) == 1 or Cn <= 1, "the channels of dy must be neighbours")
+    out = dict(dgate=torch.empty((B, L, Cn), dtype=x.dtype, device=x.device), dx=torch.empty((B, L, Cn), dtype=x.dtype, device=x.device),
+               dh0=torch.empty((B, Cn), dtype=torch.float32, device=x.device))
+    work, need = _scan_work(s, x.device)
+    _device_call(x.device, load_library().marl_linear_scan_backward, C.byref(s), _dptr(states), _dptr(dy), C.c_int64(dy.stride(0)),
+                 C.c_int64(dy.stride(1)), _dptr(dlast), _dptr(out["dgate"]), _dptr(out["dx"]), _dptr(out["dh0"]), _dptr(work), need)
+    return out
 
 
 class Actor:

@@ -1,0 +1,43 @@
+// Shared by the learner's operators (policy_logprob.cu, linear_scan.cu, orthogonalise.cu): error text, element types.
+#pragma once
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "../../include/marl_actor.h"
+
+namespace marl {
+
+int fail(int code, const char* fmt, ...);  // defined beside marl_last_error; returns code
+
+inline size_t dtype_bytes(int32_t dtype) { return dtype == MARL_DTYPE_FP32 ? 4 : 2; }
+inline bool dtype_known(int32_t dtype) { return dtype >= MARL_DTYPE_FP32 && dtype <= MARL_DTYPE_FP16; }
+inline bool misaligned(const void* p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a != 0; }
+
+// Calls f with a value of the element type.
+template <typename F>
+inline int by_dtype(int32_t dtype, F&& f) {
+  switch (dtype) {
+    case MARL_DTYPE_FP32: return f(float());
+    case MARL_DTYPE_BF16: return f(__nv_bfloat16());
+    default: return f(__half());
+  }
+}
+
+__device__ __forceinline__ float to_f32(float v) { return v; }
+__device__ __forceinline__ float to_f32(__nv_bfloat16 v) { return __bfloat162float(v); }
+__device__ __forceinline__ float to_f32(__half v) { return __half2float(v); }
+template <typename T> __device__ __forceinline__ T from_f32(float v);
+template <> __device__ __forceinline__ float from_f32<float>(float v) { return v; }
+template <> __device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
+template <> __device__ __forceinline__ __half from_f32<__half>(float v) { return __float2half_rn(v); }
+
+__device__ __forceinline__ float ex2(float v) {
+  float r;
+  asm("ex2.approx.f32 %0, %1;" : "=f"(r) : "f"(v));
+  return r;
+}
+
+}  // namespace marl

@@ -42,13 +42,14 @@ void tcs_pack_weights(int n, int D, int A, int H, int prec, const float* W1, con
 bool tcs_fast_supported(int n, int D, int A, int H, int prec);
 int launch_actor_tcs(const ActorParams& p, int sms, bool fast_gates, cudaStream_t stream);
 int launch_ring_sample(const SampleParams& p, cudaStream_t stream);
+int fail(int code, const char* fmt, ...);  // sets the text of marl_last_error (learner_util.cuh)
 }  // namespace marl
 
 using namespace marl;
 
 static thread_local std::string g_err;
 
-static int fail(int code, const char* fmt, ...) {
+int marl::fail(int code, const char* fmt, ...) {
   char buf[512];
   va_list ap;
   va_start(ap, fmt);
