@@ -467,6 +467,26 @@ int marl_linear_scan(void* stream, const marl_scan_t* in, void* y, float* last, 
 int marl_linear_scan_backward(void* stream, const marl_scan_t* in, const float* states, const void* dy, int64_t dy_b, int64_t dy_t,
                               const float* dlast, void* dgate, void* dx, float* dh0, void* work, size_t work_bytes);
 
+/* Orthogonalised updates: each matrix G of the list is replaced by scale times an approximation of the nearest matrix with orthonormal rows (or
+ * columns, if it has more rows than columns), U V' of its singular value decomposition.  X = G / (|G| + eps) with the Frobenius norm,
+ * transposed if G has more rows than columns; then `steps` times
+ *   S = X X',  X = (c0 I + c1 S + c2 S S) X
+ * with the coefficients c0, c1, c2 = coeffs[0..2] of an odd polynomial that draws singular values to 1.  What a learner does to
+ * the momentum of W1, W_ih, W_hh and W2 before it steps and publishes; all matrices of a call, of whatever shapes, share its launch.
+ * Everything is computed in fp32; a matrix of zeros gives zeros; a NaN or infinity makes its own matrix NaN. */
+#define MARL_ORTHO_MAX_SHORT 128 /* rows or columns, whichever are fewer */
+#define MARL_ORTHO_MAX_LONG 1024
+typedef struct {
+  const void* in;               /* matrix k: element (r, c) at in[k * in_batch + r * in_row + c], strides >= 0 in elements */
+  void* out;                    /* likewise; may be the input itself (same address and strides) */
+  int64_t in_batch, in_row, out_batch, out_row;
+  int32_t batch, rows, cols;    /* batch >= 0; rows, cols >= 1 */
+  float scale;
+} marl_matrix_t;
+
+/* list: HOST array of `count` entries, read before the call returns.  dtype: of all matrices.  steps 0 .. 64; eps >= 0. */
+int marl_orthogonalise(void* stream, const marl_matrix_t* list, int32_t count, int32_t dtype, int32_t steps, const float* coeffs, float eps);
+
 /* Name of the step kernel in use: "ffma" (the general path: split-operand tensor-core or CUDA-core kernel), "tcgen05"
  * (one-tile tensor-core kernel), "tcgen05-pipelined", "tcgen05-dual" (two resident tiles; its other launches run on the pipelined kernel), or
  * "tcgen05-streamed" (hidden size 128: weights kept in shared memory as far as they fit, the others streamed). */

@@ -38,6 +38,7 @@ EXPORTS = [
     "marl_actor_launch_count", "marl_last_error", "marl_rollout_noalloc", "marl_selftest_bounded_wait",
     "marl_measure_ffma_tflops", "marl_policy_logprob", "marl_policy_logprob_backward",
     "marl_linear_scan_query", "marl_linear_scan", "marl_linear_scan_backward",
+    "marl_orthogonalise",
 ]
 DTYPE = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 MAX_TOP = 32
@@ -100,6 +101,11 @@ class Scan(C.Structure):
                 ("form", C.c_int32), ("reverse", C.c_int32)]
 
 
+class Matrix(C.Structure):
+    _fields_ = [("in_", C.c_void_p), ("out", C.c_void_p), ("in_batch", C.c_int64), ("in_row", C.c_int64), ("out_batch", C.c_int64),
+                ("out_row", C.c_int64), ("batch", C.c_int32), ("rows", C.c_int32), ("cols", C.c_int32), ("scale", C.c_float)]
+
+
 class Counters(C.Structure):
     _fields_ = [("agent_steps", C.c_uint64), ("episodes", C.c_uint64), ("explored", C.c_uint64),
                 ("no_avail", C.c_uint64), ("truncated", C.c_uint64)]
@@ -152,6 +158,7 @@ def load_library():
         lib.marl_actor_reset.argtypes = [P]
         lib.marl_policy_logprob.argtypes = [P, C.POINTER(PolicyRows), C.c_int32, P, P, P, P, P]
         lib.marl_policy_logprob_backward.argtypes = [P, C.POINTER(PolicyRows), P, P, P, P, P, C.c_int64]
+        lib.marl_orthogonalise.argtypes = [P, C.POINTER(Matrix), C.c_int32, C.c_int32, C.c_int32, C.POINTER(C.c_float), C.c_float]
         lib.marl_linear_scan_query.argtypes = [C.POINTER(Scan), C.POINTER(C.c_size_t), C.POINTER(C.c_size_t)]
         lib.marl_linear_scan.argtypes = [P, C.POINTER(Scan), P, P, P, P, C.c_size_t]
         lib.marl_linear_scan_backward.argtypes = [P, C.POINTER(Scan), P, P, C.c_int64, C.c_int64, P, P, P, P, P, C.c_size_t]
@@ -372,6 +379,38 @@ def marl_linear_scan_backward(gate, x, states, dy, dlast=None, h0=None, done=Non
     _device_call(x.device, load_library().marl_linear_scan_backward, C.byref(s), _dptr(states), _dptr(dy), C.c_int64(dy.stride(0)),
                  C.c_int64(dy.stride(1)), _dptr(dlast), _dptr(out["dgate"]), _dptr(out["dx"]), _dptr(out["dh0"]), _dptr(work), need)
     return out
+
+
+def marl_orthogonalise(mats, steps: int = 5, coeffs=(3.4445, -4.7750, 2.0315), eps: float = 1e-7, scale=1.0, out=None) -> list:
+    """Orthogonalised updates of a list of matrices [r, c] or batches of them [k, r, c] (one dtype; rows may be strided), in one
+    call.  scale: one factor, or one for each entry of the list.  out: a list of tensors like mats (the same ones: in place).
+    Returns the list of results."""
+    mats = list(mats)
+    if not mats:
+        return []
+    dev, dt = mats[0].device, mats[0].dtype
+    _need(mats[0].is_cuda, "matrices must be CUDA tensors: there is no CPU path")
+    _need(dt in DTYPE, "matrices must be float32, bfloat16 or float16")
+    _need(len(coeffs) == 3, "coeffs must be three numbers")
+    outs = [torch.empty(m.shape, dtype=dt, device=dev) for m in mats] if out is None else list(out)
+    scales = [float(s) for s in scale] if isinstance(scale, (list, tuple)) else [float(scale)] * len(mats)
+    _need(len(outs) == len(mats) == len(scales), "out and scale must be as long as the list")
+    arr = (Matrix * len(mats))()
+    for e, m, o, s in zip(arr, mats, outs, scales):
+        _need(m.dim() in (2, 3) and m.numel() > 0, "a matrix has shape [r, c] or [k, r, c]")
+        _need(m.device == dev and o.device == dev, "the matrices are not all on one device")
+        _need(m.dtype == dt and o.dtype == dt and o.shape == m.shape, "the matrices must share a dtype, and out must be like them")
+        for t in (m, o):
+            _need(t.stride(-1) == 1 or t.shape[-1] == 1, "the entries of a row must be neighbours")
+        e.in_, e.out, e.in_row, e.out_row = m.data_ptr(), o.data_ptr(), m.stride(-2), o.stride(-2)
+        if m.dim() == 3:
+            e.batch, e.in_batch, e.out_batch = m.shape[0], m.stride(0), o.stride(0)
+        else:
+            e.batch = 1
+        e.rows, e.cols, e.scale = m.shape[-2], m.shape[-1], s
+    _device_call(dev, load_library().marl_orthogonalise, arr, C.c_int32(len(mats)), C.c_int32(DTYPE[dt]), C.c_int32(steps),
+                 (C.c_float * 3)(*coeffs), C.c_float(eps))
+    return outs
 
 
 class Actor:

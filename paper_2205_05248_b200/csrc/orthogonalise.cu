@@ -1,0 +1,363 @@
+// Orthogonalised updates by Newton-Schulz products: X = G / |G|, then X <- (c0 I + c1 S + c2 S S) X with S = X X', a few times.
+//
+// A matrix of up to 128 x 1024 (short side m, long side n) belongs to a cluster of 1 to 8 blocks and stays in its shared memory from the
+// load to the store: each block holds a slice of the long side, transposed (XT[j][i] = X[i][j], rows of the slice by
+// columns of the short side).  A step is
+//   each block's share of S from its slice                           -> all blocks add their rows of S up (in rank order)
+//   each block its rows of Q = c0 I + c1 S + c2 S S                   -> handed to all blocks
+//   each block XT <- XT Q on its slice, in place (a row of XT depends on that row alone)
+// The products are plain fp32 multiply-adds with register tiles: the polynomial's slope at 0 amplifies rounding errors of
+// small singular directions (c0^5 = 485), so operands of fewer bits would show in the result.
+#include "learner_util.cuh"
+#include "launch_util.cuh"
+
+#include <algorithm>
+#include <cmath>
+#include <cooperative_groups.h>
+
+namespace cg = cooperative_groups;
+
+namespace marl {
+
+constexpr int ORTHO_THREADS = 256, ORTHO_GROUPS = 32;
+constexpr int ORTHO_SMS = 148;
+
+struct OrthoGroup {
+  const void* in;
+  void* out;
+  long long in_batch, in_row, out_batch, out_row;
+  int first;       // index of its first matrix in the launch
+  int rows, cols;
+  float scale;
+};
+struct OrthoParams {
+  OrthoGroup g[ORTHO_GROUPS];
+  int groups, steps;
+  float c0, c1, c2, eps;
+};
+
+// Floats of shared memory: the slice, S, and S's share or Q.
+__host__ __device__ constexpr int padded_short(int m) { return m <= 16 ? 16 : m <= 32 ? 32 : m <= 64 ? 64 : 128; }
+__host__ __device__ constexpr int pitch_of(int mp) { return mp + 4; }  // rows start 16 bytes further round the banks
+__host__ __device__ inline int slice_of(int n, int cluster) { return ((n + cluster - 1) / cluster + 3) / 4 * 4; }
+inline size_t ortho_smem(int m, int n, int cluster) {
+  const int mp = padded_short(m);
+  return 4 * ((size_t)slice_of(n, cluster) * pitch_of(mp) + 2 * (size_t)mp * mp);
+}
+
+// Columns of a 16-wide grid of threads: groups of four neighbours 64 apart where a thread has eight, so that a warp's 16-byte loads
+// meet every bank once.
+template <int W>
+__device__ __forceinline__ int col_of(int t, int i) { return W <= 4 ? t * W + i : (i >> 2) * 64 + t * 4 + (i & 3); }
+template <int W>
+__device__ __forceinline__ void load_cols(const float* row, int t, float (&v)[W]) {
+  if constexpr (W >= 4) {
+#pragma unroll
+    for (int i = 0; i < W; i += 4) *reinterpret_cast<float4*>(&v[i]) = *reinterpret_cast<const float4*>(row + col_of<W>(t, i));
+  } else {
+#pragma unroll
+    for (int i = 0; i < W; ++i) v[i] = row[t * W + i];
+  }
+}
+template <int W>
+__device__ __forceinline__ void store_cols(float* row, int t, const float (&v)[W]) {
+  if constexpr (W >= 4) {
+#pragma unroll
+    for (int i = 0; i < W; i += 4) *reinterpret_cast<float4*>(row + col_of<W>(t, i)) = *reinterpret_cast<const float4*>(&v[i]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < W; ++i) row[t * W + i] = v[i];
+  }
+}
+
+// out[r][c] = sum over k of a[k][r0 + r] a[k][c] for r < R of this thread's rows, four neighbouring columns.
+template <int MP, int R>
+__device__ __forceinline__ void square_rows(const float* a, const int (&rows)[R], int c, float (&acc)[R][4]) {
+#pragma unroll
+  for (int r = 0; r < R; ++r) acc[r][0] = acc[r][1] = acc[r][2] = acc[r][3] = 0.f;
+#pragma unroll 8
+  for (int k = 0; k < MP; ++k) {
+    const float4 b = *reinterpret_cast<const float4*>(a + k * MP + c);
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      const float v = a[k * MP + rows[r]];
+      acc[r][0] = fmaf(v, b.x, acc[r][0]);
+      acc[r][1] = fmaf(v, b.y, acc[r][1]);
+      acc[r][2] = fmaf(v, b.z, acc[r][2]);
+      acc[r][3] = fmaf(v, b.w, acc[r][3]);
+    }
+  }
+}
+
+template <typename T, int MP>
+__device__ void ortho_matrix(const OrthoParams& p, const OrthoGroup& g, int index, float* smem) {
+  constexpr int PITCH = pitch_of(MP), W = MP / 16;
+  cg::cluster_group cluster = cg::this_cluster();
+  const int rank = (int)cluster.block_rank(), size = (int)cluster.num_blocks();
+  const bool tall = g.rows > g.cols;
+  const int m = tall ? g.cols : g.rows, n = tall ? g.rows : g.cols;
+  const int ns = slice_of(n, size), j0 = rank * ns;
+  const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;
+  float* xt = smem;                       // [ns][PITCH]
+  float* share = xt + ns * PITCH;         // [MP][MP] this block's share of S, then Q
+  float* s = share + MP * MP;             // [MP][MP]
+  __shared__ float exchange[2];           // largest modulus, sum of squares of the slice
+  __shared__ float red[ORTHO_THREADS / 32];
+
+  // load, transposed where the rows are the short side; zeros behind the matrix
+  const T* in = reinterpret_cast<const T*>(g.in) + (long long)index * g.in_batch;
+  for (int i = tid; i < ns * PITCH; i += ORTHO_THREADS) xt[i] = 0.f;
+  __syncthreads();
+  const int live = max(0, min(ns, n - j0));
+  float top = 0.f;
+  const int fast = tall ? m : live, slow = tall ? live : m;
+  for (int b = tid / 32; b < slow; b += ORTHO_THREADS / 32)
+    for (int a = tid & 31; a < fast; a += 32) {
+      const int i = tall ? a : b, j = tall ? b : a;
+      const float v = to_f32(tall ? in[(long long)(j0 + j) * g.in_row + i] : in[(long long)i * g.in_row + j0 + j]);
+      xt[j * PITCH + i] = v;
+      const float t = fabsf(v);
+      top = t > top || t != t ? t : top;  // (a NaN stays, whatever comes behind it)
+    }
+  auto block_reduce = [&](float v, auto op) {
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) v = op(v, __shfl_xor_sync(~0u, v, d));
+    if ((tid & 31) == 0) red[tid >> 5] = v;
+    __syncthreads();
+    v = red[0];
+    for (int w = 1; w < ORTHO_THREADS / 32; ++w) v = op(v, red[w]);
+    __syncthreads();
+    return v;
+  };
+  auto larger = [](float a, float b) { return a != a ? a : b != b ? b : fmaxf(a, b); };
+  auto plus = [](float a, float b) { return a + b; };
+  // |G| relative to its largest entry, so that squares neither overflow nor vanish
+  top = block_reduce(top, larger);
+  if (tid == 0) exchange[0] = top;
+  cluster.sync();
+  for (int r = 0; r < size; ++r) top = larger(top, *cluster.map_shared_rank(&exchange[0], r));
+  const float inv_top = top > 0.f ? 1.f / top : 0.f;
+  const bool tiny = top > 0.f && !(inv_top <= 3e38f);  // (1 / top overflows for the smallest subnormals: divide)
+  float sum = 0.f;
+  for (int i = tid; i < live * MP; i += ORTHO_THREADS) {
+    const int j = i / MP, c = i - j * MP;
+    const float v = tiny ? xt[j * PITCH + c] / top : xt[j * PITCH + c] * inv_top;
+    sum += v * v;
+  }
+  sum = block_reduce(sum, plus);
+  if (tid == 0) exchange[1] = sum;
+  cluster.sync();
+  sum = 0.f;
+  for (int r = 0; r < size; ++r) sum += *cluster.map_shared_rank(&exchange[1], r);
+  const float norm = top * sqrtf(sum) + p.eps;
+  for (int i = tid; i < live * MP; i += ORTHO_THREADS) {
+    const int j = i / MP, c = i - j * MP;
+    float& v = xt[j * PITCH + c];
+    v = top == 0.f ? 0.f : v / norm;
+  }
+  if (p.steps == 0) cluster.sync();  // (a block must not end while others read its sum)
+  __syncthreads();
+
+  const int rs = MP / size, row0 = rank * rs;    // this block's rows of S and Q
+  for (int step = 0; step < p.steps; ++step) {
+    {  // this block's share of S
+      float acc[W][W];
+#pragma unroll
+      for (int i = 0; i < W; ++i)
+#pragma unroll
+        for (int j = 0; j < W; ++j) acc[i][j] = 0.f;
+#pragma unroll 4
+      for (int k = 0; k < ns; ++k) {
+        float a[W], b[W];
+        load_cols<W>(xt + k * PITCH, ty, a);
+        load_cols<W>(xt + k * PITCH, tx, b);
+#pragma unroll
+        for (int i = 0; i < W; ++i)
+#pragma unroll
+          for (int j = 0; j < W; ++j) acc[i][j] = fmaf(a[i], b[j], acc[i][j]);
+      }
+#pragma unroll
+      for (int i = 0; i < W; ++i) store_cols<W>(share + col_of<W>(ty, i) * MP, tx, acc[i]);
+    }
+    cluster.sync();
+    for (int i = tid; i < rs * MP / 4; i += ORTHO_THREADS) {
+      float4 t = make_float4(0.f, 0.f, 0.f, 0.f);
+      for (int r = 0; r < size; ++r) {
+        const float4 o = reinterpret_cast<const float4*>(cluster.map_shared_rank(share, r) + row0 * MP)[i];
+        t.x += o.x;
+        t.y += o.y;
+        t.z += o.z;
+        t.w += o.w;
+      }
+      for (int r = 0; r < size; ++r) reinterpret_cast<float4*>(cluster.map_shared_rank(s, r) + row0 * MP)[i] = t;
+    }
+    cluster.sync();
+    {  // this block's rows of Q, to every block
+      constexpr int CG = MP / 4, RG = ORTHO_THREADS / CG;   // groups of four columns, threads along the rows
+      const int c = (tid % CG) * 4, r = tid / CG;
+      auto rows_of_q = [&](auto count) {
+        constexpr int R = decltype(count)::value;
+        for (int b = r; b < rs; b += RG * R) {
+          int rows[R];
+          float acc[R][4];
+#pragma unroll
+          for (int i = 0; i < R; ++i) rows[i] = row0 + min(b + i * RG, rs - 1);
+          square_rows<MP, R>(s, rows, c, acc);
+#pragma unroll
+          for (int i = 0; i < R; ++i) {
+            if (b + i * RG >= rs) continue;
+            const float4 a = *reinterpret_cast<const float4*>(s + rows[i] * MP + c);
+            const float e[4] = {a.x, a.y, a.z, a.w};
+            float q[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) q[j] = fmaf(p.c2, acc[i][j], p.c1 * e[j]) + (c + j == rows[i] ? p.c0 : 0.f);
+            for (int o = 0; o < size; ++o)
+              *reinterpret_cast<float4*>(cluster.map_shared_rank(share, o) + rows[i] * MP + c) = make_float4(q[0], q[1], q[2], q[3]);
+          }
+        }
+      };
+      if (rs >= 4 * RG) rows_of_q(std::integral_constant<int, 4>());
+      else if (rs >= 2 * RG) rows_of_q(std::integral_constant<int, 2>());
+      else rows_of_q(std::integral_constant<int, 1>());
+    }
+    cluster.sync();
+    // XT <- XT Q: the 16 threads of a row are lanes of one warp, so a row is read by them all before any of them writes it
+    constexpr int R = 4;
+    for (int b = ty * R; b < ns; b += 16 * R) {
+      float acc[R][W];
+#pragma unroll
+      for (int i = 0; i < R; ++i)
+#pragma unroll
+        for (int j = 0; j < W; ++j) acc[i][j] = 0.f;
+#pragma unroll 2
+      for (int k = 0; k < MP; k += 4) {
+        float a[R][4];
+#pragma unroll
+        for (int i = 0; i < R; ++i) *reinterpret_cast<float4*>(a[i]) = *reinterpret_cast<const float4*>(xt + (b + i) * PITCH + k);
+#pragma unroll
+        for (int kk = 0; kk < 4; ++kk) {
+          float q[W];
+          load_cols<W>(share + (k + kk) * MP, tx, q);
+#pragma unroll
+          for (int i = 0; i < R; ++i)
+#pragma unroll
+            for (int j = 0; j < W; ++j) acc[i][j] = fmaf(a[i][kk], q[j], acc[i][j]);
+        }
+      }
+      __syncwarp(0xFFFFu << (tid & 16));
+#pragma unroll
+      for (int i = 0; i < R; ++i) store_cols<W>(xt + (b + i) * PITCH, tx, acc[i]);
+    }
+    __syncthreads();
+  }
+
+  T* out = reinterpret_cast<T*>(g.out) + (long long)index * g.out_batch;
+  for (int b = tid / 32; b < slow; b += ORTHO_THREADS / 32)
+    for (int a = tid & 31; a < fast; a += 32) {
+      const int i = tall ? a : b, j = tall ? b : a;
+      T* at = tall ? out + (long long)(j0 + j) * g.out_row + i : out + (long long)i * g.out_row + j0 + j;
+      *at = from_f32<T>(g.scale * xt[j * PITCH + i]);
+    }
+}
+
+template <typename T>
+__global__ void __launch_bounds__(ORTHO_THREADS, 1) orthogonalise_kernel(const __grid_constant__ OrthoParams p) {
+  extern __shared__ __align__(16) float ortho_smem_buf[];
+  const int matrix = (int)(blockIdx.x / cg::this_cluster().num_blocks());
+  int at = 0;
+  while (at + 1 < p.groups && matrix >= p.g[at + 1].first) ++at;
+  const OrthoGroup& g = p.g[at];
+  const int m = min(g.rows, g.cols), index = matrix - g.first;
+  if (m <= 16) ortho_matrix<T, 16>(p, g, index, ortho_smem_buf);
+  else if (m <= 32) ortho_matrix<T, 32>(p, g, index, ortho_smem_buf);
+  else if (m <= 64) ortho_matrix<T, 64>(p, g, index, ortho_smem_buf);
+  else ortho_matrix<T, 128>(p, g, index, ortho_smem_buf);
+}
+
+static uint32_t g_ortho_smem[3][SMEM_OPTIN_DEVICES];
+
+template <typename T>
+static int launch_ortho(const OrthoParams& p, int matrices, int cluster, size_t smem, int which, cudaStream_t stream) {
+  auto* kernel = &orthogonalise_kernel<T>;
+  cudaError_t e = ensure_dynamic_smem(reinterpret_cast<const void*>(kernel), (uint32_t)smem, g_ortho_smem[which]);
+  if (e != cudaSuccess) return fail(MARL_ECUDA, "marl_orthogonalise: %s", cudaGetErrorString(e));
+  cudaLaunchConfig_t c = {};
+  c.gridDim = dim3((unsigned)(matrices * cluster));
+  c.blockDim = dim3(ORTHO_THREADS);
+  c.dynamicSmemBytes = smem;
+  c.stream = stream;
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeClusterDimension;
+  at[0].val.clusterDim.x = (unsigned)cluster;
+  at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+  c.attrs = at;
+  c.numAttrs = 1;
+  e = cudaLaunchKernelEx(&c, kernel, p);
+  return e == cudaSuccess ? MARL_OK : fail(MARL_ECUDA, "marl_orthogonalise: %s", cudaGetErrorString(e));
+}
+
+}  // namespace marl
+
+using namespace marl;
+
+extern "C" int marl_orthogonalise(void* stream, const marl_matrix_t* list, int32_t count, int32_t dtype, int32_t steps, const float* coeffs,
+                                  float eps) {
+  if (count < 0 || (count > 0 && !list)) return fail(MARL_EINVAL, "the list is NULL or its length negative");
+  if (!dtype_known(dtype)) return fail(MARL_EINVAL, "unknown dtype %d", dtype);
+  if (steps < 0 || steps > 64) return fail(MARL_EINVAL, "steps must be in [0, 64]");
+  if (!coeffs) return fail(MARL_EINVAL, "coeffs is NULL");
+  if (!(eps >= 0.f) || !std::isfinite(eps)) return fail(MARL_EINVAL, "eps must be >= 0 and finite");
+  for (int i = 0; i < count; ++i) {
+    const marl_matrix_t& g = list[i];
+    if (g.batch < 0) return fail(MARL_EINVAL, "matrix %d: batch is negative", i);
+    if (g.rows < 1 || g.cols < 1 || std::min(g.rows, g.cols) > MARL_ORTHO_MAX_SHORT || std::max(g.rows, g.cols) > MARL_ORTHO_MAX_LONG)
+      return fail(MARL_EINVAL, "matrix %d: %d x %d is outside 1 x 1 .. %d x %d (either way round)", i, g.rows, g.cols, MARL_ORTHO_MAX_SHORT,
+                  MARL_ORTHO_MAX_LONG);
+    if (g.batch == 0) continue;
+    if (!g.in || !g.out) return fail(MARL_EINVAL, "matrix %d: in or out is NULL", i);
+    if (g.in_batch < 0 || g.in_row < 0) return fail(MARL_EINVAL, "matrix %d: a stride is negative", i);
+    if ((g.rows > 1 && g.out_row < g.cols) || (g.batch > 1 && g.out_batch < (g.rows - 1) * g.out_row + g.cols))
+      return fail(MARL_EINVAL, "matrix %d: rows or matrices of the output overlap", i);
+    if (misaligned(g.in, dtype_bytes(dtype)) || misaligned(g.out, dtype_bytes(dtype)))
+      return fail(MARL_EALIGN, "matrix %d is not aligned to its elements", i);
+  }
+  for (int i0 = 0; i0 < count;) {
+    OrthoParams p = {};
+    p.steps = steps;
+    p.c0 = coeffs[0];
+    p.c1 = coeffs[1];
+    p.c2 = coeffs[2];
+    p.eps = eps;
+    long long matrices = 0;
+    int i = i0;
+    for (; i < count && p.groups < ORTHO_GROUPS; ++i) {
+      const marl_matrix_t& g = list[i];
+      if (g.batch == 0) continue;
+      if (matrices + g.batch > (1 << 24)) {
+        if (p.groups == 0) return fail(MARL_EINVAL, "matrix %d: batch is larger than 2^24", i);
+        break;
+      }
+      p.g[p.groups++] = OrthoGroup{g.in, g.out, g.in_batch, g.in_row, g.out_batch, g.out_row, (int)matrices, g.rows, g.cols, g.scale};
+      matrices += g.batch;
+    }
+    auto smem_for = [&](int cluster) {
+      size_t need = 0;
+      for (int k = 0; k < p.groups; ++k)
+        need = std::max(need, ortho_smem(std::min(p.g[k].rows, p.g[k].cols), std::max(p.g[k].rows, p.g[k].cols), cluster));
+      return need;
+    };
+    i0 = i;
+    if (p.groups == 0) continue;
+    // Few matrices: as many blocks a matrix as the device has room for; more: as few as their shared memory allows.
+    int cluster = 1;
+    while (cluster < 8 && smem_for(cluster) > 200 * 1024) cluster *= 2;
+    while (cluster < 8 && matrices * cluster * 2 <= ORTHO_SMS) cluster *= 2;
+    const size_t smem = smem_for(cluster);
+    int rc;
+    if (dtype == MARL_DTYPE_FP32) rc = launch_ortho<float>(p, (int)matrices, cluster, smem, 0, (cudaStream_t)stream);
+    else if (dtype == MARL_DTYPE_BF16) rc = launch_ortho<__nv_bfloat16>(p, (int)matrices, cluster, smem, 1, (cudaStream_t)stream);
+    else rc = launch_ortho<__half>(p, (int)matrices, cluster, smem, 2, (cudaStream_t)stream);
+    if (rc != MARL_OK) return rc;
+  }
+  return MARL_OK;
+}

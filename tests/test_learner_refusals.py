@@ -145,3 +145,40 @@ def test_scan_tensors_without_a_gpu_are_refused():
     x = torch.zeros(2, 3, 4)
     with pytest.raises(binding.MarlError):
         binding.marl_linear_scan(x, x)
+
+
+def _matrix(**over):
+    p = dict(in_=GOOD, out=GOOD, in_batch=64, in_row=8, out_batch=64, out_row=8, batch=2, rows=8, cols=8, scale=1.0)
+    p.update(over)
+    return binding.Matrix(*[p[k] for k, _ in binding.Matrix._fields_])
+
+
+def _ortho(lib, entries, count=None, dtype=0, steps=5, coeffs=(3.4, -4.7, 2.0), eps=1e-7):
+    arr = (binding.Matrix * max(1, len(entries)))(*entries)
+    co = (C.c_float * 3)(*coeffs) if coeffs is not None else None
+    return lib.marl_orthogonalise(None, arr, len(entries) if count is None else count, dtype, steps, co, eps)
+
+
+@pytest.mark.parametrize("over,code", [
+    (dict(batch=-1), EINVAL), (dict(rows=0), EINVAL), (dict(cols=0), EINVAL), (dict(rows=129, cols=129), EINVAL),
+    (dict(rows=1025, cols=4), EINVAL), (dict(rows=4, cols=1025), EINVAL), (dict(in_=None), EINVAL), (dict(out=None), EINVAL),
+    (dict(in_row=-1), EINVAL), (dict(in_batch=-1), EINVAL), (dict(out_row=7), EINVAL), (dict(out_batch=63), EINVAL),
+    (dict(in_=GOOD + 2), EALIGN), (dict(out=GOOD + 2), EALIGN)])
+def test_matrices_are_refused(lib, over, code):
+    assert _ortho(lib, [_matrix(**over)]) == code and lib.marl_last_error()
+    assert _ortho(lib, [_matrix(batch=0), _matrix(**over)]) == code
+
+
+def test_orthogonalise_arguments_are_refused(lib):
+    m = [_matrix()]
+    assert _ortho(lib, m, dtype=3) == EINVAL and _ortho(lib, m, steps=-1) == EINVAL and _ortho(lib, m, steps=65) == EINVAL
+    assert _ortho(lib, m, eps=-1.0) == EINVAL and _ortho(lib, m, eps=float("nan")) == EINVAL and _ortho(lib, m, eps=float("inf")) == EINVAL
+    assert _ortho(lib, m, coeffs=None) == EINVAL and _ortho(lib, m, count=-1) == EINVAL
+    assert lib.marl_orthogonalise(None, None, 1, 0, 5, (C.c_float * 3)(1, 1, 1), 0.0) == EINVAL
+    assert _ortho(lib, []) == 0 and _ortho(lib, [_matrix(batch=0, in_=None, out=None)]) == 0
+
+
+def test_matrices_without_a_gpu_are_refused():
+    with pytest.raises(binding.MarlError):
+        binding.marl_orthogonalise([torch.zeros(4, 4)])
+    assert binding.marl_orthogonalise([]) == []
