@@ -6,11 +6,16 @@
 #include "learner_util.cuh"
 #include "launch_util.cuh"
 
+#include <algorithm>
 #include <cmath>
+#include <cooperative_groups.h>
+
+namespace cg = cooperative_groups;
 
 namespace marl {
 
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
+constexpr int LOGPROB_SMS = 148;
 constexpr int KEY_NONE = INT32_MIN;          // no entry
 constexpr int KEY_NEG_INF = (int)0x807FFFFF;  // the key of -infinity: entries rank above it
 
@@ -26,6 +31,8 @@ struct RowsParams {
   float2* stats;
   int32_t* top_index;
   float* top_logp;
+  int parts;   // blocks a row
+  int fours;   // the alternatives are written four at a time
 };
 
 struct RowsGradParams {
@@ -40,6 +47,12 @@ struct RowsGradParams {
 __device__ __forceinline__ float max_nan(float a, float b) {
   float r;
   asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
+
+__device__ __forceinline__ float max3_nan(float a, float b, float c) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
   return r;
 }
 
@@ -74,8 +87,17 @@ __device__ __forceinline__ Sums join(Sums a, Sums b, float c) {
   a.v += b.v;
   return a;
 }
-__device__ __forceinline__ Sums shuffle(const Sums& a, int mask) {
-  return Sums{__shfl_xor_sync(~0u, a.m, mask), __shfl_xor_sync(~0u, a.s, mask), __shfl_xor_sync(~0u, a.v, mask)};
+// The sums of all lanes, in every lane.
+__device__ __forceinline__ void join_lanes(Sums& a, float c) {
+  float m = a.m;
+#pragma unroll
+  for (int d = 16; d > 0; d >>= 1) m = max_nan(m, __shfl_xor_sync(~0u, m, d));
+  rescale(a, m, c);
+#pragma unroll
+  for (int d = 16; d > 0; d >>= 1) {
+    a.s += __shfl_xor_sync(~0u, a.s, d);
+    a.v += __shfl_xor_sync(~0u, a.v, d);
+  }
 }
 
 // The row's results from its sums; x_a = the taken action's value if available, -infinity if it is not.
@@ -115,59 +137,64 @@ __device__ __forceinline__ void merge_list(Entry& a, const Entry& b, int lane) {
   for (int j = 16; j > 0; j >>= 1) exchange(a, lane, j, true);
 }
 
-// A warp's list while it walks its part of a row in ascending order of indexes, 32 * N values at a time.  `worst` is the top-th entry;
-// *shared holds the largest such key of the row's warps: an entry below it cannot be among the row's best.
+// Puts the values of the warp (lane l: v[0..N) at indexes i0 .. i0 + N - 1) that are at least `floor_key` into its list of the best 32;
+// the top-th entry of the list decides what still enters.  Called by the whole warp.
 template <int N>
-struct TopWalk {
-  Entry mine, worst;
-  float bar;  // values not above it cannot enter
-  __device__ __forceinline__ void reset() {
-    mine = worst = entry_none();
-    bar = -INFINITY;
-  }
-  __device__ __forceinline__ void raise(int shared_key) {
-    int b = worst.key > KEY_NEG_INF ? worst.key : KEY_NEG_INF;
-    if (shared_key - 1 > b) b = shared_key - 1;
-    bar = b == INT32_MAX ? INFINITY : key_value(b);  // (as many NaN as entries: nothing enters behind them)
-  }
-  // Values of lane l: v[0..N) at indexes i0 .. i0 + N - 1 (i0 ascending with the lane).  Called by the whole warp.
-  __device__ __noinline__ void take(const float (&v)[N], int i0, int lane, int top, int* shared) {
-    unsigned used = 0;
-    int sk = *(volatile int*)shared;
-    while (true) {
-      Entry c = entry_none();
-      int cj = 0;
+__device__ __forceinline__ void take(Entry& mine, const float (&v)[N], int i0, int lane, int top, int floor_key) {
+  unsigned used = 0;
+  while (true) {
+    const Entry worst = shfl_entry(mine, top - 1);
+    Entry c = entry_none();
+    int cj = 0;
 #pragma unroll
-      for (int j = 0; j < N; ++j) {
-        const int k = order_key(v[j]);
-        if (!(used >> j & 1) && k > c.key) {
-          c = Entry{k, i0 + j};
-          cj = j;
-        }
+    for (int j = 0; j < N; ++j) {
+      const int k = order_key(v[j]);
+      if (!(used >> j & 1) && k > c.key) {
+        c = Entry{k, i0 + j};
+        cj = j;
       }
-      const bool in = c.key > KEY_NEG_INF && c.key >= sk && better(c, worst);
-      unsigned who = __ballot_sync(~0u, in);
-      if (!who) break;
-      if (in) used |= 1u << cj;
-      if (__popc(who) <= 4) {  // one by one
-        for (; who; who &= who - 1) {
-          const Entry n = shfl_entry(c, __ffs(who) - 1);
-          const int pos = __popc(__ballot_sync(~0u, better(mine, n)));
-          const Entry up{__shfl_up_sync(~0u, mine.key, 1), __shfl_up_sync(~0u, mine.idx, 1)};
-          if (lane == pos) mine = n;
-          else if (lane > pos) mine = up;
-        }
-      } else {                 // the lanes' candidates sorted, then merged into the list
-        Entry s = in ? c : entry_none();
-        sort_list(s, lane);
-        merge_list(mine, s, lane);
-      }
-      worst = shfl_entry(mine, top - 1);
     }
-    if (lane == 0 && worst.key > sk) atomicMax(shared, worst.key);
-    raise(sk);
+    const bool in = c.key > KEY_NEG_INF && c.key >= floor_key && better(c, worst);
+    unsigned who = __ballot_sync(~0u, in);
+    if (!who) return;
+    if (in) used |= 1u << cj;
+    if (__popc(who) <= 4) {  // one by one
+      for (; who; who &= who - 1) {
+        const Entry n = shfl_entry(c, __ffs(who) - 1);
+        const int pos = __popc(__ballot_sync(~0u, better(mine, n)));
+        const Entry up{__shfl_up_sync(~0u, mine.key, 1), __shfl_up_sync(~0u, mine.idx, 1)};
+        if (lane == pos) mine = n;
+        else if (lane > pos) mine = up;
+      }
+    } else {                 // the lanes' candidates sorted, then merged into the list
+      Entry s = in ? c : entry_none();
+      sort_list(s, lane);
+      merge_list(mine, s, lane);
+    }
   }
-};
+}
+
+// The lanes' keys in descending order.
+__device__ __forceinline__ int sort_keys(int key, int lane) {
+#pragma unroll
+  for (int k = 2; k <= 32; k <<= 1)
+#pragma unroll
+    for (int j = k >> 1; j > 0; j >>= 1) {
+      const int o = __shfl_xor_sync(~0u, key, j);
+      key = ((lane & j) == 0) == ((lane & k) == 0) ? max(key, o) : min(key, o);
+    }
+  return key;
+}
+// The 32 largest of two descending lists, descending; `other` is read backwards.
+__device__ __forceinline__ int merge_keys(int key, int other_reversed, int lane) {
+  key = max(key, other_reversed);
+#pragma unroll
+  for (int j = 16; j > 0; j >>= 1) {
+    const int o = __shfl_xor_sync(~0u, key, j);
+    key = (lane & j) == 0 ? max(key, o) : min(key, o);
+  }
+  return key;
+}
 
 // ---- 16 bytes of a row and their availability -----------------------------------------------------------------------
 template <typename T> struct Vec;
@@ -215,90 +242,187 @@ __device__ __forceinline__ void load_avail(const uint8_t* a, uint32_t (&w)[N / 4
   for (int i = 0; i < N / 4; ++i) w[i] = __funnelshift_r(r[i], r[i + 1], sh);
 }
 
+// Two sums side by side (even and odd elements), in the packed fp32 arithmetic of the device.
+struct Sums2 {
+  float m;
+  float2 s, v;
+};
+__device__ __forceinline__ void add_values(Sums2& a, float x0, float x1, float m, float c) {
+  float2 u = mul2(add2(make_float2(x0, x1), make_float2(-m, -m)), make_float2(c, c));
+  u.x = max_nan(u.x, -200.f);
+  u.y = max_nan(u.y, -200.f);
+  const float2 e = make_float2(ex2(u.x), ex2(u.y));
+  a.s = add2(a.s, e);
+  a.v = fma2(e, u, a.v);
+}
 template <int N>
-__device__ __forceinline__ void add_values(Sums& a, const float (&v)[N], float c, float& largest) {
-  float top = v[0];
+__device__ __forceinline__ void add_values(Sums2& a, const float (&v)[N], float c) {
+  float top = max_nan(v[0], v[1]);
 #pragma unroll
-  for (int j = 1; j < N; ++j) top = max_nan(top, v[j]);
-  largest = top;
-  if (!(top <= a.m)) rescale(a, max_nan(top, a.m), c);  // (also when top is NaN)
+  for (int j = 2; j < N; j += 2) top = max3_nan(top, v[j], v[j + 1]);
+  if (!(top <= a.m)) {  // (also when top is NaN)
+    Sums x{a.m, a.s.x, a.v.x}, y{a.m, a.s.y, a.v.y};
+    top = max_nan(top, a.m);
+    rescale(x, top, c);
+    rescale(y, top, c);
+    a = Sums2{top, make_float2(x.s, y.s), make_float2(x.v, y.v)};
+  }
   const float m = base_of(a.m);
 #pragma unroll
-  for (int j = 0; j < N; ++j) {
-    const float u = exponent(v[j], m, c), e = ex2(u);
-    a.s += e;
-    a.v += e * u;
-  }
+  for (int j = 0; j < N; j += 2) add_values(a, v[j], v[j + 1], m, c);
 }
 
 // ---- rows of more than SMALL_A actions ------------------------------------------------------------------------------
-// WARPS warps of a block walk a row together, 16 bytes a lane, each warp every WARPS-th group of 512 bytes; with WARPS = 1 a block holds eight
-// rows.  A row that starts off a 16-byte boundary has up to 15 bytes in front and behind that its first and last warp
-// take element by element.
+// WARPS warps of a block walk a row together, 16 bytes a lane, each warp every WARPS-th group of 512 bytes; with WARPS = 1 a block holds
+// eight rows.  Few rows are divided over the blocks of a cluster in the same way.  A row that starts off a 16-byte boundary has up to 15
+// bytes in front and behind that the first and the last warp take element by element.
+// The alternatives cost the pass nothing: each lane knows the largest value that it has met, and the top-th largest of a block's such
+// values is met or exceeded by at least `top` entries of the row.  Behind the pass only the lanes whose largest value reaches
+// that bar are walked again, by their whole warp, from the cache.
 constexpr int WIDE_THREADS = 256;
 
 template <typename T, int WARPS, bool TOP, bool MASK>
 __global__ void __launch_bounds__(WIDE_THREADS) logprob_wide_kernel(const __grid_constant__ RowsParams p) {
   constexpr int N = Vec<T>::N, ROWS = WIDE_THREADS / 32 / WARPS;
   const int lane = threadIdx.x & 31, warp = (threadIdx.x >> 5) % WARPS, sub = (threadIdx.x >> 5) / WARPS;
-  const long long row = (long long)blockIdx.x * ROWS + sub;
-  __shared__ int shared_key[ROWS];
-  __shared__ Sums part[WARPS];
-  __shared__ Entry lists[TOP && WARPS > 1 ? WARPS : 1][32];
-  if (threadIdx.x < ROWS) shared_key[threadIdx.x] = KEY_NONE + 1;
-  __syncthreads();
+  const int parts = WARPS > 1 ? p.parts : 1, rank = WARPS > 1 ? (int)(blockIdx.x % parts) : 0;
+  const long long row = WARPS > 1 ? (long long)blockIdx.x / parts : (long long)blockIdx.x * ROWS + sub;
   if (row >= p.rows) return;  // (WARPS = 1 only: no barrier follows)
   const T* x = reinterpret_cast<const T*>(p.x) + row * p.xs;
   const uint8_t* av = MASK ? p.avail + row * p.as : nullptr;
   const int off = (int)((16 - (reinterpret_cast<uintptr_t>(x) & 15)) & 15) / (int)sizeof(T);
   const int head = off < p.A ? off : p.A, body = (p.A - head) / N, tail = p.A - head - body * N;
+  const int stride = 32 * WARPS * parts, first = (rank * WARPS + warp) * 32;
+  const bool does_head = head && first == 0, does_tail = tail && rank == parts - 1 && warp == WARPS - 1;
 
-  Sums a{-INFINITY, 0.f, 0.f};
-  TopWalk<N> walk;
-  if (TOP) walk.reset();
-  float v[N], largest;
-  auto one_by_one = [&](int i0, int n) {  // n < N elements from i0 on, one per lane
+  Sums2 a2{-INFINITY, make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+  const uint4* xv = reinterpret_cast<const uint4*>(x + head);
+  auto load_one = [&](int i0, int n, float (&v)[N]) {  // n < N elements from i0 on, one a lane
 #pragma unroll
     for (int j = 0; j < N; ++j) v[j] = -INFINITY;
     if (lane < n && (!MASK || av[i0 + lane])) v[0] = to_f32(x[i0 + lane]);
-    add_values<N>(a, v, p.c, largest);
-    if (TOP && __any_sync(~0u, !(largest <= walk.bar))) walk.take(v, i0 + lane, lane, p.top, &shared_key[sub]);
   };
-  if (head && warp == 0) one_by_one(0, head);
-  const uint4* xv = reinterpret_cast<const uint4*>(x + head);
-#pragma unroll 2
-  for (int g = warp * 32; g < body; g += 32 * WARPS) {
-    const int i = g + lane, i0 = head + i * N;
-    if (i < body) {
-      Vec<T>::unpack(__ldg(xv + i), v);
-      if (MASK) {
-        uint32_t w[N / 4];
-        load_avail<N>(av + i0, w);
+  auto hide = [&](int i, float (&v)[N]) {
+    uint32_t w[N / 4];
+    load_avail<N>(av + head + (long long)i * N, w);
 #pragma unroll
-        for (int j = 0; j < N; ++j)
-          if (!(w[j / 4] >> (8 * (j & 3)) & 0xFF)) v[j] = -INFINITY;
-      }
-    } else {
-#pragma unroll
-      for (int j = 0; j < N; ++j) v[j] = -INFINITY;
-    }
-    add_values<N>(a, v, p.c, largest);
-    if (TOP && __any_sync(~0u, !(largest <= walk.bar))) walk.take(v, i0, lane, p.top, &shared_key[sub]);
+    for (int j = 0; j < N; ++j)
+      if (!(w[j / 4] >> (8 * (j & 3)) & 0xFF)) v[j] = -INFINITY;
+  };
+  if (does_head) {
+    float v[N];
+    load_one(0, head, v);
+    add_values<N>(a2, v, p.c);
   }
-  if (tail && warp == WARPS - 1) one_by_one(head + body * N, tail);
-
+  int i = first + lane;
+  for (; i + 3 * stride < body; i += 4 * stride) {  // four loads on their way at a time
+    uint4 r[4];
 #pragma unroll
-  for (int m = 16; m > 0; m >>= 1) a = join(a, shuffle(a, m), p.c);
+    for (int k = 0; k < 4; ++k) r[k] = __ldg(xv + i + k * stride);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      float v[N];
+      Vec<T>::unpack(r[k], v);
+      if (MASK) hide(i + k * stride, v);
+      add_values<N>(a2, v, p.c);
+    }
+  }
+  for (; i < body; i += stride) {
+    float v[N];
+    Vec<T>::unpack(__ldg(xv + i), v);
+    if (MASK) hide(i, v);
+    add_values<N>(a2, v, p.c);
+  }
+  __syncwarp();
+  if (does_tail) {
+    float v[N];
+    load_one(head + body * N, tail, v);
+    add_values<N>(a2, v, p.c);
+  }
+
+  const float lane_max = a2.m;
+  Sums a{a2.m, a2.s.x + a2.s.y, a2.v.x + a2.v.y};
+  join_lanes(a, p.c);
+  __shared__ Sums part[WARPS];
+  __shared__ int keys[TOP && WARPS > 1 ? WARPS : 1][32];
+  __shared__ Entry lists[TOP && WARPS > 1 ? WARPS : 1][32];
+  const int mine_key = TOP ? order_key(lane_max) : 0;
+  int bar = TOP ? sort_keys(mine_key, lane) : 0;
   if (WARPS > 1) {
     if (lane == 0) part[warp] = a;
-    if (TOP) lists[warp][lane] = walk.mine;
-    __syncthreads();
-    if (warp) return;
-#pragma unroll 1
-    for (int w = 1; w < WARPS; ++w) {
-      a = join(a, part[w], p.c);
-      if (TOP) merge_list(walk.mine, lists[w][lane], lane);
+    if (TOP) {
+#pragma unroll
+      for (int w = 1; w < WARPS; w *= 2) {  // pairs of warps, pairs of pairs ...
+        if (warp % (2 * w) == w) keys[warp][lane] = bar;
+        __syncthreads();
+        if (warp % (2 * w) == 0) bar = merge_keys(bar, keys[warp + w][31 - lane], lane);
+      }
+      if (warp == 0 && lane == p.top - 1) keys[0][0] = bar;
     }
+    __syncthreads();
+    if (TOP) bar = keys[0][0];
+  } else if (TOP) bar = __shfl_sync(~0u, bar, p.top - 1);
+  Entry best = entry_none();
+  if (TOP) {
+    float v[N];
+    if (does_head) {
+      load_one(0, head, v);
+      take(best, v, lane, lane, p.top, bar);
+    }
+    // the walk of a lane is `steps` vectors, `stride` apart: as many lanes' as fit are read again at a time
+    unsigned who = __ballot_sync(~0u, mine_key >= bar && mine_key > KEY_NEG_INF);
+    const int steps = first < body ? (body - first + stride - 1) / stride : 0;
+    int lg = 0;
+    while ((1 << lg) < steps && lg < 5) ++lg;
+    while (who) {
+      unsigned m = who;
+      for (int k = lane >> lg; k && m; --k) m &= m - 1;
+      const int l = m ? __ffs(m) - 1 : 0;
+      for (int s0 = 0; s0 < steps; s0 += 1 << lg) {
+        const long long k = first + l + (long long)(s0 + (lane & ((1 << lg) - 1))) * stride;
+        if (m && k < body) {
+          Vec<T>::unpack(__ldg(xv + k), v);
+          if (MASK) hide((int)k, v);
+        } else {
+#pragma unroll
+          for (int j = 0; j < N; ++j) v[j] = -INFINITY;
+        }
+        take(best, v, head + (int)k * N, lane, p.top, bar);
+      }
+      for (int k = 32 >> lg; k && who; --k) who &= who - 1;
+    }
+    if (does_tail) {
+      load_one(head + body * N, tail, v);
+      take(best, v, head + body * N + lane, lane, p.top, bar);
+    }
+  }
+  if (WARPS > 1) {
+    if (TOP) lists[warp][lane] = best;
+    __syncthreads();
+    if (warp == 0) {
+#pragma unroll 1
+      for (int w = 1; w < WARPS; ++w) {
+        a = join(a, part[w], p.c);
+        if (TOP) merge_list(best, lists[w][lane], lane);
+      }
+    }
+    if (parts > 1) {  // the blocks' sums and lists, in the order of their ranks
+      cg::cluster_group cluster = cg::this_cluster();
+      if (warp == 0) {
+        if (lane == 0) part[0] = a;
+        if (TOP) lists[0][lane] = best;
+      }
+      cluster.sync();
+      if (rank == 0 && warp == 0) {
+        for (int r = 1; r < parts; ++r) {
+          a = join(a, *cluster.map_shared_rank(&part[0], r), p.c);
+          if (TOP) merge_list(best, *cluster.map_shared_rank(&lists[0][lane], r), lane);
+        }
+      }
+      cluster.sync();
+      if (rank) return;
+    }
+    if (warp) return;
   }
   if (lane == 0) {
     const int act = p.action[row];
@@ -306,28 +430,66 @@ __global__ void __launch_bounds__(WIDE_THREADS) logprob_wide_kernel(const __grid
     write_row(p, row, a, has, has && (!MASK || av[act]) ? to_f32(x[act]) : -INFINITY);
   }
   if (TOP && lane < p.top) {
-    const Entry e = walk.mine;
-    const bool some = e.key > KEY_NEG_INF;
-    p.top_index[row * p.top + lane] = some ? e.idx : -1;
-    p.top_logp[row * p.top + lane] = some ? (to_f32(x[e.idx]) - a.m) * p.it - logf(a.s) : -INFINITY;
+    const bool some = best.key > KEY_NEG_INF;
+    p.top_index[row * p.top + lane] = some ? best.idx : -1;
+    p.top_logp[row * p.top + lane] = some ? (to_f32(x[best.idx]) - a.m) * p.it - logf(a.s) : -INFINITY;
   }
 }
 
 // ---- rows of up to SMALL_A actions ----------------------------------------------------------------------------------
-// A thread per row: 128 rows come in element by element, neighbouring threads neighbouring elements, and are laid out in shared memory an
-// odd number of words apart, so that the threads' walks over their rows meet no bank twice.
+// A thread per row: 128 rows come in with neighbouring threads on neighbouring elements and are laid out in shared memory an odd number of
+// words apart, so that the threads' walks over their rows meet no bank twice.  DENSE: rows without gaps on 16-byte boundaries (the q of a
+// sampled batch) come in four elements a load.
 constexpr int SMALL_A = 32, SMALL_ROWS = 128;
 
-template <typename T, int MA>
+// i / A for i < 4096, A <= 32: inv = ceil(2^20 / A).
+__device__ __forceinline__ int div_small(int i, uint32_t inv) { return (int)((uint32_t)i * inv >> 20); }
+
+template <typename T> struct Four;
+template <> struct Four<float> {
+  static __device__ __forceinline__ void load(const float* at, float (&v)[4]) { *reinterpret_cast<float4*>(v) = *reinterpret_cast<const float4*>(at); }
+  static __device__ __forceinline__ void store(float* at, const float (&v)[4]) { *reinterpret_cast<float4*>(at) = *reinterpret_cast<const float4*>(v); }
+};
+template <typename T> struct Four16 {
+  static __device__ __forceinline__ void load(const T* at, float (&v)[4]) {
+    const uint2 r = *reinterpret_cast<const uint2*>(at);
+    const T* e = reinterpret_cast<const T*>(&r);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) v[k] = to_f32(e[k]);
+  }
+  static __device__ __forceinline__ void store(T* at, const float (&v)[4]) {
+    uint2 r;
+    T* e = reinterpret_cast<T*>(&r);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) e[k] = from_f32<T>(v[k]);
+    *reinterpret_cast<uint2*>(at) = r;
+  }
+};
+template <> struct Four<__nv_bfloat16> : Four16<__nv_bfloat16> {};
+template <> struct Four<__half> : Four16<__half> {};
+
+template <typename T, int MA, bool DENSE>
 __global__ void __launch_bounds__(SMALL_ROWS) logprob_small_kernel(const __grid_constant__ RowsParams p, uint32_t inv_a) {
   __shared__ float xs[SMALL_ROWS * (MA + 1)];
   const long long row0 = (long long)blockIdx.x * SMALL_ROWS;
-  const int rows = (int)(p.rows - row0 < SMALL_ROWS ? p.rows - row0 : SMALL_ROWS), A = p.A, pitch = A | 1;
+  const int rows = (int)(p.rows - row0 < SMALL_ROWS ? p.rows - row0 : SMALL_ROWS), A = p.A, pitch = A | 1, pad = pitch - A;
   const T* x = reinterpret_cast<const T*>(p.x) + row0 * p.xs;
   const uint8_t* av = p.avail ? p.avail + row0 * p.as : nullptr;
-#pragma unroll 8
-  for (int i = threadIdx.x; i < rows * A; i += SMALL_ROWS) {
-    const int r = (int)((uint32_t)i * inv_a >> 20), j = i - r * A;  // i / A: inv_a = ceil(2^20 / A), i < 4096, A <= 32
+  const int total = rows * A, fours = DENSE ? total >> 2 : 0;
+#pragma unroll 4
+  for (int q = threadIdx.x; q < fours; q += SMALL_ROWS) {
+    float v[4];
+    Four<T>::load(x + 4 * q, v);
+    const uint32_t w = av ? __ldg(reinterpret_cast<const uint32_t*>(av) + q) : 0x01010101u;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int i = 4 * q + e;
+      xs[i + pad * div_small(i, inv_a)] = w >> (8 * e) & 0xFF ? v[e] : -INFINITY;
+    }
+  }
+#pragma unroll 4
+  for (int i = 4 * fours + threadIdx.x; i < total; i += SMALL_ROWS) {
+    const int r = div_small(i, inv_a), j = i - r * A;
     float v = to_f32(x[r * p.xs + j]);
     if (av && !av[r * p.as + j]) v = -INFINITY;
     xs[r * pitch + j] = v;
@@ -343,103 +505,225 @@ __global__ void __launch_bounds__(SMALL_ROWS) logprob_small_kernel(const __grid_
     v[j] = j < A ? mine[j] : -INFINITY;
     m = max_nan(m, v[j]);
   }
-  Sums a{m, 0.f, 0.f};
+  Sums2 a2{m, make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
   const float b = base_of(m);
 #pragma unroll
-  for (int j = 0; j < MA; ++j) {
-    const float u = exponent(v[j], b, p.c), e = ex2(u);
-    a.s += e;
-    a.v += e * u;
-  }
+  for (int j = 0; j < MA; j += 2) add_values(a2, v[j], v[j + 1], b, p.c);
+  const Sums a{m, a2.s.x + a2.s.y, a2.v.x + a2.v.y};
   const long long row = row0 + r;
   const int act = p.action[row];
   const bool has = act >= 0 && act < A;
   write_row(p, row, a, has, has ? mine[act] : -INFINITY);
   if (!p.top) return;
   const float ls = logf(a.s);
-  unsigned used = 0;
-  for (int k = 0; k < p.top; ++k) {
-    int bk = KEY_NEG_INF, bj = -1;
+  if (m != m) {  // a NaN ranks above all numbers: +infinity in its place, and that below it
 #pragma unroll
-    for (int j = 0; j < MA; ++j) {
-      const int key = order_key(v[j]);
-      if (key > bk && !(used >> j & 1)) {
-        bk = key;
-        bj = j;
-      }
+    for (int j = 0; j < MA; ++j) v[j] = v[j] != v[j] ? INFINITY : v[j] == INFINITY ? 3.402823466e38f : v[j];
+  }
+  int out_j[4];
+  float out_l[4];
+  for (int k0 = 0; k0 < p.top; k0 += 4) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      float top = -INFINITY;
+      int bj = -1;
+#pragma unroll
+      for (int j = 0; j < MA; ++j)
+        if (v[j] > top) {
+          top = v[j];
+          bj = j;
+        }
+#pragma unroll
+      for (int j = 0; j < MA; ++j)
+        if (j == bj) v[j] = -INFINITY;
+      out_j[k] = bj;
+      out_l[k] = bj >= 0 ? (mine[bj] - a.m) * p.it - ls : -INFINITY;
+      if (k0 + k + 1 >= p.top) break;
     }
-    used |= bj >= 0 ? 1u << bj : 0u;
-    p.top_index[row * p.top + k] = bj;
-    p.top_logp[row * p.top + k] = bj >= 0 ? (mine[bj] - a.m) * p.it - ls : -INFINITY;
+    int* ti = p.top_index + row * p.top + k0;
+    float* tl = p.top_logp + row * p.top + k0;
+    if (p.fours) {
+      *reinterpret_cast<int4*>(ti) = *reinterpret_cast<int4*>(out_j);
+      *reinterpret_cast<float4*>(tl) = *reinterpret_cast<float4*>(out_l);
+    } else {
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if (k0 + k < p.top) {
+          ti[k] = out_j[k];
+          tl[k] = out_l[k];
+        }
+    }
   }
 }
 
 // ---- gradient -------------------------------------------------------------------------------------------------------
+// With l = log2 p_j: dx_j = -p_j (k + h l), and g more at the action taken; k = g + h entropy, h in natural units of l.
 struct RowGrad {
-  float m, ls2, gl, ge, ent2;  // largest value, log2 S, gradients over T, entropy in bits
-  int action;
-  bool empty;
+  float m, ls2, k, h, g;  // largest value, log2 S
+  int action;             // -1: none
 };
 __device__ __forceinline__ RowGrad row_grad(const RowsGradParams& q, long long row) {
   const float2 st = q.r.stats[row];
-  RowGrad g;
-  g.empty = st.y == -INFINITY;
-  g.m = st.x;
-  g.ls2 = st.y * LOG2E;
+  RowGrad r{0.f, 0.f, 0.f, 0.f, 0.f, -1};
+  if (st.y == -INFINITY) return r;  // an empty row: nothing in it is available
   const int act = q.r.action[row];
-  const bool has = act >= 0 && act < q.r.A;
-  g.action = has ? act : -1;
-  g.gl = q.g_logp && has ? q.g_logp[row] * q.r.it : 0.f;
-  g.ge = q.g_entropy ? q.g_entropy[row] * q.r.it * LN2 : 0.f;
-  g.ent2 = q.r.entropy[row] * LOG2E;
-  return g;
+  if (act >= 0 && act < q.r.A) {
+    r.action = act;
+    r.g = q.g_logp ? q.g_logp[row] * q.r.it : 0.f;
+  }
+  const float h = q.g_entropy ? q.g_entropy[row] * q.r.it : 0.f;
+  r.m = st.x;
+  r.ls2 = st.y * LOG2E;
+  r.h = h * LN2;
+  r.k = r.g + h * q.r.entropy[row];
+  return r;
 }
-// x of an available entry.
-__device__ __forceinline__ float entry_grad(const RowGrad& g, float x, int j, float c) {
-  const float l = max_nan((x - g.m) * c - g.ls2, -200.f), pr = ex2(l);
-  float d = -pr * (g.gl + g.ge * (l + g.ent2));
-  if (j == g.action) d += g.gl;
-  return d;
+// x of an available entry, or -infinity: 0 then.
+__device__ __forceinline__ float entry_grad(float m, float ls2, float k, float h, float x, float c) {
+  const float l = max_nan((x - m) * c - ls2, -200.f);
+  return -ex2(l) * fmaf(h, l, k);
 }
 
-// A warp per segment of a row, neighbouring lanes neighbouring elements.
-template <typename T>
+// A warp per segment of a row of more than SMALL_A actions, 16 bytes of the gradient a lane.  Where the logits' rows lie otherwise than the
+// gradient's from a 16-byte boundary, each lane takes its logits from the two aligned vectors that hold them, the second from the
+// lane behind it.
+template <typename T, bool MASK>
 __global__ void __launch_bounds__(256) logprob_wide_grad_kernel(const __grid_constant__ RowsGradParams q) {
+  constexpr int N = Vec<T>::N;
   const int lane = threadIdx.x & 31;
   const long long unit = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
   const long long row = unit / q.segments;
   if (row >= q.r.rows) return;
-  const int j0 = (int)(unit - row * q.segments) * q.seg_len;
-  const int j1 = q.r.A - j0 < q.seg_len ? q.r.A : j0 + q.seg_len;
+  const int segment = (int)(unit - row * q.segments), A = q.r.A;
   const RowGrad g = row_grad(q, row);
   const T* x = reinterpret_cast<const T*>(q.r.x) + row * q.r.xs;
-  const uint8_t* av = q.r.avail ? q.r.avail + row * q.r.as : nullptr;
+  const uint8_t* av = MASK ? q.r.avail + row * q.r.as : nullptr;
   T* d = reinterpret_cast<T*>(q.dx) + row * q.ds;
-#pragma unroll 8
-  for (int j = j0 + lane; j < j1; j += 32) {
-    const float v = to_f32(x[j]);
-    const bool on = !g.empty && v != -INFINITY && (!av || av[j]);
-    d[j] = from_f32<T>(on ? entry_grad(g, v, j, q.r.c) : 0.f);
+  const float c = q.r.c;
+  const int off = (int)((16 - (reinterpret_cast<uintptr_t>(d) & 15)) & 15) / (int)sizeof(T);
+  const int head = off < A ? off : A, body = (A - head) / N, tail = A - head - body * N;
+  auto single = [&](int j) {
+    float v = to_f32(x[j]);
+    if (MASK && !av[j]) v = -INFINITY;
+    float o = entry_grad(g.m, g.ls2, g.k, g.h, v, c);
+    if (j == g.action && v != -INFINITY) o += g.g;
+    d[j] = from_f32<T>(o);
+  };
+  if (segment == 0 && lane < head) single(lane);
+  if (segment == q.segments - 1 && lane < tail) single(head + body * N + lane);
+  const int i0 = segment * q.seg_len, i1 = min(body, i0 + q.seg_len);  // vectors
+  const uintptr_t xa = reinterpret_cast<uintptr_t>(x + head);
+  const uint4* xv = reinterpret_cast<const uint4*>(xa & ~(uintptr_t)15);
+  const int shift = (int)(xa & 15);                                    // bytes
+  constexpr int BATCH = 4;  // vectors on their way at a time (the gradient may be written over the logits: no load moves up past a store)
+  for (int b = i0; b < i1; b += 32 * BATCH) {
+    uint4 raw[BATCH], next[BATCH];
+    uint32_t w[BATCH][N / 4];
+#pragma unroll
+    for (int k = 0; k < BATCH; ++k) {
+      const int i = b + 32 * k + lane;
+      raw[k] = next[k] = make_uint4(0u, 0u, 0u, 0u);
+      if (i >= i1) continue;
+      raw[k] = *(xv + i);
+      if (shift && (lane == 31 || i + 1 == i1)) next[k] = *(xv + i + 1);
+      if (MASK) load_avail<N>(av + head + i * N, w[k]);
+    }
+#pragma unroll
+    for (int k = 0; k < BATCH; ++k) {
+      const int i = b + 32 * k + lane;
+      uint4 r = raw[k];
+      if (shift) {
+        uint4 n{__shfl_down_sync(~0u, r.x, 1), __shfl_down_sync(~0u, r.y, 1), __shfl_down_sync(~0u, r.z, 1), __shfl_down_sync(~0u, r.w, 1)};
+        if (lane == 31 || i + 1 == i1) n = next[k];
+        uint32_t t[8] = {r.x, r.y, r.z, r.w, n.x, n.y, n.z, n.w};
+        if (shift & 8) {
+#pragma unroll
+          for (int e = 0; e < 6; ++e) t[e] = t[e + 2];
+        }
+        if (shift & 4) {
+#pragma unroll
+          for (int e = 0; e < 5; ++e) t[e] = t[e + 1];
+        }
+        const int sh = (shift & 3) * 8;
+        r = make_uint4(__funnelshift_r(t[0], t[1], sh), __funnelshift_r(t[1], t[2], sh), __funnelshift_r(t[2], t[3], sh), __funnelshift_r(t[3], t[4], sh));
+      }
+      if (i >= i1) continue;
+      float v[N], o[N];
+      Vec<T>::unpack(r, v);
+      const int j0 = head + i * N;
+      if (MASK) {
+#pragma unroll
+        for (int j = 0; j < N; ++j)
+          if (!(w[k][j / 4] >> (8 * (j & 3)) & 0xFF)) v[j] = -INFINITY;
+      }
+#pragma unroll
+      for (int j = 0; j < N; ++j) o[j] = entry_grad(g.m, g.ls2, g.k, g.h, v[j], c);
+      if ((unsigned)(g.action - j0) < (unsigned)N) {
+#pragma unroll
+        for (int j = 0; j < N; ++j)
+          if (j0 + j == g.action && v[j] != -INFINITY) o[j] += g.g;
+      }
+      uint4 s;
+      T* e = reinterpret_cast<T*>(&s);
+#pragma unroll
+      for (int j = 0; j < N; ++j) e[j] = from_f32<T>(o[j]);
+      reinterpret_cast<uint4*>(d + head)[i] = s;
+    }
   }
 }
 
-// 128 rows a block, neighbouring threads neighbouring elements.
-template <typename T>
+// 128 rows a block, neighbouring threads on neighbouring elements, four at a time where all rows are dense.
+template <typename T, bool DENSE>
 __global__ void __launch_bounds__(SMALL_ROWS) logprob_small_grad_kernel(const __grid_constant__ RowsGradParams q, uint32_t inv_a) {
-  __shared__ RowGrad gs[SMALL_ROWS];
+  __shared__ float4 gs[SMALL_ROWS];
+  __shared__ float2 chosen[SMALL_ROWS];  // gradient, and place (as bits) of the action taken in the block's rows laid end to end
   const long long row0 = (long long)blockIdx.x * SMALL_ROWS;
   const int rows = (int)(q.r.rows - row0 < SMALL_ROWS ? q.r.rows - row0 : SMALL_ROWS), A = q.r.A;
-  if ((int)threadIdx.x < rows) gs[threadIdx.x] = row_grad(q, row0 + threadIdx.x);
+  if ((int)threadIdx.x < rows) {
+    const RowGrad g = row_grad(q, row0 + threadIdx.x);
+    gs[threadIdx.x] = make_float4(g.m, g.ls2, g.k, g.h);
+    chosen[threadIdx.x] = make_float2(g.g, __int_as_float(g.action >= 0 ? (int)threadIdx.x * A + g.action : -1));
+  }
   __syncthreads();
   const T* x = reinterpret_cast<const T*>(q.r.x) + row0 * q.r.xs;
   const uint8_t* av = q.r.avail ? q.r.avail + row0 * q.r.as : nullptr;
   T* d = reinterpret_cast<T*>(q.dx) + row0 * q.ds;
-#pragma unroll 8
-  for (int i = threadIdx.x; i < rows * A; i += SMALL_ROWS) {
-    const int r = (int)((uint32_t)i * inv_a >> 20), j = i - r * A;
-    const float v = to_f32(x[r * q.r.xs + j]);
-    const bool on = !gs[r].empty && v != -INFINITY && (!av || av[r * q.r.as + j]);
-    d[r * q.ds + j] = from_f32<T>(on ? entry_grad(gs[r], v, j, q.r.c) : 0.f);
+  auto gradient = [&](float v, int r, int i) {
+    const float4 g = gs[r];
+    const float2 t = chosen[r];
+    float o = entry_grad(g.x, g.y, g.z, g.w, v, q.r.c);
+    if (__float_as_int(t.y) == i && v != -INFINITY) o += t.x;
+    return o;
+  };
+  const int total = rows * A, fours = DENSE ? total >> 2 : 0;
+  constexpr int BATCH = 4;
+  for (int b = threadIdx.x; b < fours; b += BATCH * SMALL_ROWS) {
+    float v[BATCH][4];
+    uint32_t w[BATCH];
+#pragma unroll
+    for (int k = 0; k < BATCH; ++k) {
+      const int i = b + k * SMALL_ROWS;
+      if (i >= fours) break;
+      Four<T>::load(x + 4 * i, v[k]);
+      w[k] = av ? reinterpret_cast<const uint32_t*>(av)[i] : 0x01010101u;
+    }
+#pragma unroll
+    for (int k = 0; k < BATCH; ++k) {
+      const int i = b + k * SMALL_ROWS;
+      if (i >= fours) break;
+      float o[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        o[e] = gradient(w[k] >> (8 * e) & 0xFF ? v[k][e] : -INFINITY, div_small(4 * i + e, inv_a), 4 * i + e);
+      Four<T>::store(d + 4 * i, o);
+    }
+  }
+#pragma unroll 4
+  for (int i = 4 * fours + threadIdx.x; i < total; i += SMALL_ROWS) {
+    const int r = div_small(i, inv_a), j = i - r * A;
+    float v = to_f32(x[r * q.r.xs + j]);
+    if (av && !av[r * q.r.as + j]) v = -INFINITY;
+    d[r * q.ds + j] = from_f32<T>(gradient(v, r, i));
   }
 }
 
@@ -477,21 +761,46 @@ static int launched(const char* what) {
   return e == cudaSuccess ? MARL_OK : fail(MARL_ECUDA, "%s: %s", what, cudaGetErrorString(e));
 }
 
+// Rows without gaps, on boundaries that four elements and four bytes of availability need.
+template <typename T>
+static bool rows_dense(const RowsParams& p) {
+  return p.xs == p.A && !misaligned(p.x, 4 * sizeof(T)) && (!p.avail || (p.as == p.A && !misaligned(p.avail, 4)));
+}
+
 template <typename T>
 static int launch_logprob(const RowsParams& p, cudaStream_t stream) {
   if (p.A <= SMALL_A) {
     const long long blocks = (p.rows + SMALL_ROWS - 1) / SMALL_ROWS;
     if (blocks > INT32_MAX) return fail(MARL_EINVAL, "too many rows");
     const uint32_t inv = ((1u << 20) + p.A - 1) / p.A;
-    if (p.A <= 8) logprob_small_kernel<T, 8><<<(unsigned)blocks, SMALL_ROWS, 0, stream>>>(p, inv);
-    else if (p.A <= 16) logprob_small_kernel<T, 16><<<(unsigned)blocks, SMALL_ROWS, 0, stream>>>(p, inv);
-    else logprob_small_kernel<T, 32><<<(unsigned)blocks, SMALL_ROWS, 0, stream>>>(p, inv);
+    RowsParams q = p;
+    q.fours = p.top % 4 == 0 && !misaligned(p.top_index, 16) && !misaligned(p.top_logp, 16);
+    const bool dense = rows_dense<T>(p);
+    auto go = [&](auto kernel) { kernel<<<(unsigned)blocks, SMALL_ROWS, 0, stream>>>(q, inv); };
+    if (p.A <= 8) dense ? go(logprob_small_kernel<T, 8, true>) : go(logprob_small_kernel<T, 8, false>);
+    else if (p.A <= 16) dense ? go(logprob_small_kernel<T, 16, true>) : go(logprob_small_kernel<T, 16, false>);
+    else dense ? go(logprob_small_kernel<T, 32, true>) : go(logprob_small_kernel<T, 32, false>);
     return launched("marl_policy_logprob");
   }
   const bool warp_rows = p.A <= 2048;
-  const long long blocks = warp_rows ? (p.rows + 7) / 8 : p.rows;
+  RowsParams q = p;
+  q.parts = 1;
+  if (!warp_rows)
+    while (q.parts < 8 && p.rows * q.parts * 2 <= 2 * LOGPROB_SMS && p.A / (q.parts * 2) >= 4096) q.parts *= 2;
+  const long long blocks = warp_rows ? (p.rows + 7) / 8 : p.rows * q.parts;
   if (blocks > INT32_MAX) return fail(MARL_EINVAL, "too many rows");
-  auto go = [&](auto kernel) { kernel<<<(unsigned)blocks, WIDE_THREADS, 0, stream>>>(p); };
+  cudaLaunchConfig_t lc = {};
+  lc.gridDim = dim3((unsigned)blocks);
+  lc.blockDim = dim3(WIDE_THREADS);
+  lc.stream = stream;
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeClusterDimension;
+  at[0].val.clusterDim.x = (unsigned)q.parts;
+  at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+  lc.attrs = at;
+  lc.numAttrs = q.parts > 1 ? 1 : 0;
+  cudaError_t err = cudaSuccess;
+  auto go = [&](auto kernel) { err = cudaLaunchKernelEx(&lc, kernel, q); };
   if (warp_rows) {
     if (p.top) p.avail ? go(logprob_wide_kernel<T, 1, true, true>) : go(logprob_wide_kernel<T, 1, true, false>);
     else p.avail ? go(logprob_wide_kernel<T, 1, false, true>) : go(logprob_wide_kernel<T, 1, false, false>);
@@ -499,6 +808,7 @@ static int launch_logprob(const RowsParams& p, cudaStream_t stream) {
     if (p.top) p.avail ? go(logprob_wide_kernel<T, 8, true, true>) : go(logprob_wide_kernel<T, 8, true, false>);
     else p.avail ? go(logprob_wide_kernel<T, 8, false, true>) : go(logprob_wide_kernel<T, 8, false, false>);
   }
+  if (err != cudaSuccess) return fail(MARL_ECUDA, "marl_policy_logprob: %s", cudaGetErrorString(err));
   return launched("marl_policy_logprob");
 }
 
@@ -507,14 +817,18 @@ static int launch_logprob_grad(RowsGradParams q, cudaStream_t stream) {
   if (q.r.A <= SMALL_A) {
     const long long blocks = (q.r.rows + SMALL_ROWS - 1) / SMALL_ROWS;
     if (blocks > INT32_MAX) return fail(MARL_EINVAL, "too many rows");
-    logprob_small_grad_kernel<T><<<(unsigned)blocks, SMALL_ROWS, 0, stream>>>(q, ((1u << 20) + q.r.A - 1) / q.r.A);
+    const uint32_t inv = ((1u << 20) + q.r.A - 1) / q.r.A;
+    if (rows_dense<T>(q.r) && q.ds == q.r.A && !misaligned(q.dx, 4 * sizeof(T)))
+      logprob_small_grad_kernel<T, true><<<(unsigned)blocks, SMALL_ROWS, 0, stream>>>(q, inv);
+    else logprob_small_grad_kernel<T, false><<<(unsigned)blocks, SMALL_ROWS, 0, stream>>>(q, inv);
     return launched("marl_policy_logprob_backward");
   }
-  q.seg_len = 2048;
-  q.segments = (q.r.A + q.seg_len - 1) / q.seg_len;
+  q.seg_len = q.r.A > 32768 ? 1024 : 256;
+  q.segments = std::max(1, (q.r.A / Vec<T>::N + q.seg_len - 1) / q.seg_len);
   const long long units = q.r.rows * q.segments, blocks = (units + 7) / 8;
   if (blocks > INT32_MAX) return fail(MARL_EINVAL, "too many rows");
-  logprob_wide_grad_kernel<T><<<(unsigned)blocks, 256, 0, stream>>>(q);
+  if (q.r.avail) logprob_wide_grad_kernel<T, true><<<(unsigned)blocks, 256, 0, stream>>>(q);
+  else logprob_wide_grad_kernel<T, false><<<(unsigned)blocks, 256, 0, stream>>>(q);
   return launched("marl_policy_logprob_backward");
 }
 
