@@ -50,12 +50,6 @@ __device__ __forceinline__ float max_nan(float a, float b) {
   return r;
 }
 
-__device__ __forceinline__ float max3_nan(float a, float b, float c) {
-  float r;
-  asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
-  return r;
-}
-
 // An integer that orders like the value: equal for -0 and +0, NaN above +infinity.
 __device__ __forceinline__ int order_key(float v) {
   const int b = __float_as_int(v + 0.0f);
@@ -66,26 +60,20 @@ __device__ __forceinline__ float key_value(int k) {
   return __int_as_float(k ^ ((k >> 31) & 0x7FFFFFFF));
 }
 
-// Running sums of a part of a row.  Values are relative to m (to 0 while m is -infinity: every term is then 0).  Exponents below
-// 2^-200 are clamped there: such a term is 0 in fp32, and stays 0 when it is multiplied by its exponent.
+// Running sums of a part of a row, relative to the largest value m: the largest term is 1 exactly.
+// Values below a floor are raised to it, unavailable ones among them, so that no exponent is infinite (a term of 0 times an infinite exponent
+// would be NaN); m starts there.  A row whose floor is not far below its largest value - empty rows, rows of the type's lowest
+// numbers, NaN, infinities, extreme temperatures - is walked once more, carefully.
 struct Sums {
   float m, s, v;
 };
-__device__ __forceinline__ float exponent(float x, float m, float c) { return max_nan((x - m) * c, -200.f); }
-__device__ __forceinline__ float base_of(float m) { return m == -INFINITY ? 0.f : m; }
-__device__ __forceinline__ void rescale(Sums& a, float m, float c) {  // m >= a.m
-  const float d = a.m == m ? 0.f : exponent(a.m, base_of(m), c), f = ex2(d);
+// log2 of the factor between sums relative to m and to the larger m_new; 2^-200 is 0 in fp32
+__device__ __forceinline__ float step_down(float m, float m_new, float c) { return max_nan((m - m_new) * c, -200.f); }
+__device__ __forceinline__ void rescale(Sums& a, float m, float c) {
+  const float d = step_down(a.m, m, c), f = ex2(d);
   a.v = f * (a.v + d * a.s);
   a.s *= f;
   a.m = m;
-}
-__device__ __forceinline__ Sums join(Sums a, Sums b, float c) {
-  const float m = max_nan(a.m, b.m);
-  rescale(a, m, c);
-  rescale(b, m, c);
-  a.s += b.s;
-  a.v += b.v;
-  return a;
 }
 // The sums of all lanes, in every lane.
 __device__ __forceinline__ void join_lanes(Sums& a, float c) {
@@ -99,14 +87,44 @@ __device__ __forceinline__ void join_lanes(Sums& a, float c) {
     a.v += __shfl_xor_sync(~0u, a.v, d);
   }
 }
+__device__ __forceinline__ bool trusted(const Sums& a, float floor_value, float c) {
+  const float u = (floor_value - a.m) * c;
+  return u <= -150.f && u >= -1.0e38f;
+}
+// The exponent of x relative to m, by a difference that cannot overflow to the wrong side; m = -infinity: no entry has been met.
+__device__ __forceinline__ float exponent(float x, float m, float c) { return max_nan((x - (m == -INFINITY ? 0.f : m)) * c, -200.f); }
 
-// The row's results from its sums; x_a = the taken action's value if available, -infinity if it is not.
-__device__ __forceinline__ void write_row(const RowsParams& p, long long row, const Sums& a, bool has_action, float x_a) {
+// The row's results from its sums; x_a = the taken action's value if available, -infinity if it is not.  Returns log S.
+__device__ __forceinline__ float write_row(const RowsParams& p, long long row, const Sums& a, bool has_action, float x_a) {
   const bool empty = a.m == -INFINITY;
   const float ls = empty ? -INFINITY : logf(a.s);
   p.stats[row] = make_float2(a.m, ls);
   p.entropy[row] = empty ? 0.f : ls - a.v / a.s * LN2;
   p.logp[row] = empty || !has_action ? 0.f : (x_a - a.m) * p.it - ls;
+  return ls;
+}
+
+// The sums of n elements, by one warp, whatever their values.
+template <typename T>
+__device__ __noinline__ Sums careful_sums(const T* x, const uint8_t* av, int n, float c, int lane) {
+  Sums a{-INFINITY, 0.f, 0.f};
+  for (int i = lane; i < n; i += 32)
+    if (!av || av[i]) a.m = max_nan(a.m, to_f32(x[i]));
+#pragma unroll
+  for (int d = 16; d > 0; d >>= 1) a.m = max_nan(a.m, __shfl_xor_sync(~0u, a.m, d));
+  for (int i = lane; i < n; i += 32) {
+    const float v = to_f32(x[i]);
+    if ((av && !av[i]) || v == -INFINITY) continue;
+    const float u = exponent(v, a.m, c), e = ex2(u);
+    a.s += e;
+    a.v += e * u;
+  }
+#pragma unroll
+  for (int d = 16; d > 0; d >>= 1) {
+    a.s += __shfl_xor_sync(~0u, a.s, d);
+    a.v += __shfl_xor_sync(~0u, a.v, d);
+  }
+  return a;
 }
 
 // ---- the list of the best entries: one per lane of a warp, best first -----------------------------------------------
@@ -137,94 +155,168 @@ __device__ __forceinline__ void merge_list(Entry& a, const Entry& b, int lane) {
   for (int j = 16; j > 0; j >>= 1) exchange(a, lane, j, true);
 }
 
-// Puts the values of the warp (lane l: v[0..N) at indexes i0 .. i0 + N - 1) that are at least `floor_key` into its list of the best 32;
-// the top-th entry of the list decides what still enters.  Called by the whole warp.
-template <int N>
-__device__ __forceinline__ void take(Entry& mine, const float (&v)[N], int i0, int lane, int top, int floor_key) {
-  unsigned used = 0;
-  while (true) {
-    const Entry worst = shfl_entry(mine, top - 1);
-    Entry c = entry_none();
-    int cj = 0;
-#pragma unroll
-    for (int j = 0; j < N; ++j) {
-      const int k = order_key(v[j]);
-      if (!(used >> j & 1) && k > c.key) {
-        c = Entry{k, i0 + j};
-        cj = j;
-      }
-    }
-    const bool in = c.key > KEY_NEG_INF && c.key >= floor_key && better(c, worst);
-    unsigned who = __ballot_sync(~0u, in);
-    if (!who) return;
-    if (in) used |= 1u << cj;
-    if (__popc(who) <= 4) {  // one by one
-      for (; who; who &= who - 1) {
-        const Entry n = shfl_entry(c, __ffs(who) - 1);
-        const int pos = __popc(__ballot_sync(~0u, better(mine, n)));
-        const Entry up{__shfl_up_sync(~0u, mine.key, 1), __shfl_up_sync(~0u, mine.idx, 1)};
-        if (lane == pos) mine = n;
-        else if (lane > pos) mine = up;
-      }
-    } else {                 // the lanes' candidates sorted, then merged into the list
-      Entry s = in ? c : entry_none();
-      sort_list(s, lane);
-      merge_list(mine, s, lane);
-    }
+// The n-th best of the lanes' entries, in every lane.
+__device__ __forceinline__ Entry nth_best(Entry e, int n, int lane) {
+  if (n > 8) {
+    sort_list(e, lane);
+    return shfl_entry(e, n - 1);
   }
+  Entry b = entry_none();
+  for (int r = 0; r < n; ++r) {
+    b.key = __reduce_max_sync(~0u, e.key);
+    b.idx = __reduce_min_sync(~0u, e.key == b.key ? e.idx : INT32_MAX);
+    if (e.key == b.key && e.idx == b.idx) e = entry_none();
+  }
+  return b;
 }
 
-// The lanes' keys in descending order.
-__device__ __forceinline__ int sort_keys(int key, int lane) {
-#pragma unroll
-  for (int k = 2; k <= 32; k <<= 1)
-#pragma unroll
-    for (int j = k >> 1; j > 0; j >>= 1) {
-      const int o = __shfl_xor_sync(~0u, key, j);
-      key = ((lane & j) == 0) == ((lane & k) == 0) ? max(key, o) : min(key, o);
-    }
-  return key;
+// The alternatives of a row, after the pass over it.  Each lane knows the largest value that it met and the vector of N entries in which
+// it met it first: lane l has an entry of key k_l at an index below at_l + N.  Let (k, at) be one of these pairs with at least `top`
+// pairs as good as it (higher key, or equal key and at most its index).  Then at least `top` entries are as good as (k, at + N - 1), so
+// the best `top` are among those that are, and only the lanes whose pair is as good can hold one.  (A lane that met a NaN notes
+// the last vector, not the first: all such lanes count.)  Those lanes' vectors are walked again, from the cache, and the entries that pass
+// are collected: about `top` of them on values in no particular order, and no more for rows of equal values.
+struct Bar {
+  Entry e;
+  float value;
+};
+__device__ __forceinline__ Bar make_bar(const Entry& e) { return Bar{e, e.key <= KEY_NEG_INF ? -INFINITY : e.key == INT32_MAX ? NAN : key_value(e.key)}; }
+// (a lane with nothing above the floor has no pair)
+__device__ __forceinline__ Entry lane_entry(float largest, int at, float floor_value) {
+  return largest <= floor_value ? entry_none() : Entry{order_key(largest), at};
 }
-// The 32 largest of two descending lists, descending; `other` is read backwards.
-__device__ __forceinline__ int merge_keys(int key, int other_reversed, int lane) {
-  key = max(key, other_reversed);
+__device__ __forceinline__ bool reaches(const Entry& e, const Entry& bar) {
+  return bar.key <= KEY_NEG_INF || e.key > bar.key || (e.key == bar.key && (e.idx <= bar.idx || e.key == INT32_MAX));
+}
+template <int N, int CAP>
+__device__ __forceinline__ void collect(const float (&v)[N], int i0, const Bar& bar, Entry* found, int* count) {
 #pragma unroll
-  for (int j = 16; j > 0; j >>= 1) {
-    const int o = __shfl_xor_sync(~0u, key, j);
-    key = (lane & j) == 0 ? max(key, o) : min(key, o);
+  for (int j = 0; j < N; ++j)
+    if (!(v[j] < bar.value) && v[j] != -INFINITY) {
+      const Entry e{order_key(v[j]), i0 + j};
+      if (e.key > bar.e.key || (e.key == bar.e.key && e.idx - N < bar.e.idx)) {
+        const int at = atomicAdd(count, 1);  // (their order does not matter: they are sorted by value and index)
+        if (at < CAP) found[at] = e;
+      }
+    }
+}
+// The best 32 of n entries, one a lane, best first.
+__device__ __forceinline__ Entry best_of(const Entry* found, int n, int lane) {
+  Entry best = lane < n ? found[lane] : entry_none();
+  sort_list(best, lane);
+  for (int b = 32; b < n; b += 32) {
+    Entry e = b + lane < n ? found[b + lane] : entry_none();
+    sort_list(e, lane);
+    merge_list(best, e, lane);
   }
-  return key;
+  return best;
+}
+// More entries than there is room for (many large values in few lanes): the warp walks the elements [i0, i1) one by one.
+template <typename T>
+__device__ __noinline__ void walk(Entry& best, const T* x, const uint8_t* av, int i0, int i1, int top, int lane) {
+  for (int b = i0; b < i1; b += 32) {
+    const int i = b + lane;
+    Entry e = entry_none();
+    if (i < i1 && (!av || av[i])) e = Entry{order_key(to_f32(x[i])), i};
+    const Entry worst = shfl_entry(best, top - 1);
+    const bool in = e.key > KEY_NEG_INF && better(e, worst);
+    unsigned who = __ballot_sync(~0u, in);
+    if (__popc(who) > 4) {
+      if (!in) e = entry_none();
+      sort_list(e, lane);
+      merge_list(best, e, lane);
+      continue;
+    }
+    for (; who; who &= who - 1) {
+      const Entry n = shfl_entry(e, __ffs(who) - 1);
+      const int pos = __popc(__ballot_sync(~0u, better(best, n)));
+      const Entry up{__shfl_up_sync(~0u, best.key, 1), __shfl_up_sync(~0u, best.idx, 1)};
+      if (lane == pos) best = n;
+      else if (lane > pos) best = up;
+    }
+  }
 }
 
 // ---- 16 bytes of a row and their availability -----------------------------------------------------------------------
+__device__ __forceinline__ uint32_t prmt(uint32_t a, uint32_t sel) {
+  uint32_t r;
+  asm("prmt.b32 %0, %1, %1, %2;" : "=r"(r) : "r"(a), "r"(sel));
+  return r;
+}
+// The highest bit of each byte, set where the byte is not 0.
+__device__ __forceinline__ uint32_t nonzero_bytes(uint32_t w) { return ((w & 0x7F7F7F7Fu) + 0x7F7F7F7Fu) | w; }
+
+// FLOOR: what values are raised to (-2^100; for fp16 its lowest number).
 template <typename T> struct Vec;
 template <> struct Vec<float> {
   static constexpr int N = 4;
+  static constexpr uint32_t FLOOR_BITS = 0xF1800000u;
+  static __device__ __forceinline__ float floor_value() { return __uint_as_float(FLOOR_BITS); }
   static __device__ __forceinline__ void unpack(const uint4& r, float (&v)[4]) {
     v[0] = __uint_as_float(r.x); v[1] = __uint_as_float(r.y); v[2] = __uint_as_float(r.z); v[3] = __uint_as_float(r.w);
   }
-};
-template <> struct Vec<__nv_bfloat16> {
-  static constexpr int N = 8;
-  static __device__ __forceinline__ void unpack(const uint4& r, float (&v)[8]) {
-    const uint32_t w[4] = {r.x, r.y, r.z, r.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      v[2 * i] = __uint_as_float(w[i] << 16);
-      v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
-    }
+  static __device__ __forceinline__ void hide(uint4& r, const uint32_t (&w)[1]) {
+    const uint32_t t = nonzero_bytes(w[0]);
+    const uint32_t a = prmt(t, 0x8888), b = prmt(t, 0x9999), c = prmt(t, 0xAAAA), d = prmt(t, 0xBBBB);
+    r.x = (r.x & a) | (FLOOR_BITS & ~a);
+    r.y = (r.y & b) | (FLOOR_BITS & ~b);
+    r.z = (r.z & c) | (FLOOR_BITS & ~c);
+    r.w = (r.w & d) | (FLOOR_BITS & ~d);
+  }
+  static __device__ __forceinline__ uint32_t raise(uint32_t w) { return __float_as_uint(max_nan(__uint_as_float(w), floor_value())); }
+  static __device__ __forceinline__ float largest(const uint4& r) {
+    return max_nan(max_nan(__uint_as_float(r.x), __uint_as_float(r.y)), max_nan(__uint_as_float(r.z), __uint_as_float(r.w)));
   }
 };
-template <> struct Vec<__half> {
+template <typename T> struct Vec16 {
   static constexpr int N = 8;
+  static __device__ __forceinline__ void hide(uint4& r, const uint32_t (&w)[2]) {
+    constexpr uint32_t F = Vec<T>::FLOOR_BITS;
+    const uint32_t t = nonzero_bytes(w[0]), u = nonzero_bytes(w[1]);
+    const uint32_t a = prmt(t, 0x9988), b = prmt(t, 0xBBAA), c = prmt(u, 0x9988), d = prmt(u, 0xBBAA);
+    r.x = (r.x & a) | (F & ~a);
+    r.y = (r.y & b) | (F & ~b);
+    r.z = (r.z & c) | (F & ~c);
+    r.w = (r.w & d) | (F & ~d);
+  }
+  static __device__ __forceinline__ uint32_t raise(uint32_t w) { return Vec<T>::max2(w, Vec<T>::FLOOR_BITS); }
+  static __device__ __forceinline__ float largest(const uint4& r) {
+    float a, b;
+    Vec<T>::pair(Vec<T>::max2(Vec<T>::max2(r.x, r.y), Vec<T>::max2(r.z, r.w)), a, b);
+    return max_nan(a, b);
+  }
   static __device__ __forceinline__ void unpack(const uint4& r, float (&v)[8]) {
-    const uint32_t w[4] = {r.x, r.y, r.z, r.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
-      v[2 * i] = f.x;
-      v[2 * i + 1] = f.y;
-    }
+    Vec<T>::pair(r.x, v[0], v[1]);
+    Vec<T>::pair(r.y, v[2], v[3]);
+    Vec<T>::pair(r.z, v[4], v[5]);
+    Vec<T>::pair(r.w, v[6], v[7]);
+  }
+};
+template <> struct Vec<__nv_bfloat16> : Vec16<__nv_bfloat16> {
+  static constexpr uint32_t FLOOR_BITS = 0xF180F180u;
+  static __device__ __forceinline__ float floor_value() { return __uint_as_float(0xF1800000u); }
+  static __device__ __forceinline__ uint32_t max2(uint32_t a, uint32_t b) {
+    uint32_t r;
+    asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+  }
+  static __device__ __forceinline__ void pair(uint32_t w, float& a, float& b) {
+    a = __uint_as_float(w << 16);
+    b = __uint_as_float(w & 0xFFFF0000u);
+  }
+};
+template <> struct Vec<__half> : Vec16<__half> {
+  static constexpr uint32_t FLOOR_BITS = 0xFBFFFBFFu;
+  static __device__ __forceinline__ float floor_value() { return -65504.f; }
+  static __device__ __forceinline__ uint32_t max2(uint32_t a, uint32_t b) {
+    uint32_t r;
+    asm("max.NaN.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+  }
+  static __device__ __forceinline__ void pair(uint32_t w, float& a, float& b) {
+    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w));
+    a = f.x;
+    b = f.y;
   }
 };
 
@@ -242,198 +334,324 @@ __device__ __forceinline__ void load_avail(const uint8_t* a, uint32_t (&w)[N / 4
   for (int i = 0; i < N / 4; ++i) w[i] = __funnelshift_r(r[i], r[i + 1], sh);
 }
 
-// Two sums side by side (even and odd elements), in the packed fp32 arithmetic of the device.
-struct Sums2 {
+// The running sums of a lane: even and odd elements side by side, in the packed fp32 arithmetic of the device, and two of these in turn.
+// at: first element of the vector that brought the largest value so far.
+template <typename T>
+struct Run {
+  static constexpr int N = Vec<T>::N;
   float m;
-  float2 s, v;
-};
-__device__ __forceinline__ void add_values(Sums2& a, float x0, float x1, float m, float c) {
-  float2 u = mul2(add2(make_float2(x0, x1), make_float2(-m, -m)), make_float2(c, c));
-  u.x = max_nan(u.x, -200.f);
-  u.y = max_nan(u.y, -200.f);
-  const float2 e = make_float2(ex2(u.x), ex2(u.y));
-  a.s = add2(a.s, e);
-  a.v = fma2(e, u, a.v);
-}
-template <int N>
-__device__ __forceinline__ void add_values(Sums2& a, const float (&v)[N], float c) {
-  float top = max_nan(v[0], v[1]);
-#pragma unroll
-  for (int j = 2; j < N; j += 2) top = max3_nan(top, v[j], v[j + 1]);
-  if (!(top <= a.m)) {  // (also when top is NaN)
-    Sums x{a.m, a.s.x, a.v.x}, y{a.m, a.s.y, a.v.y};
-    top = max_nan(top, a.m);
-    rescale(x, top, c);
-    rescale(y, top, c);
-    a = Sums2{top, make_float2(x.s, y.s), make_float2(x.v, y.v)};
+  float2 s[2], v[2];
+  int at;
+  __device__ __forceinline__ Run() {
+    m = Vec<T>::floor_value();
+    s[0] = s[1] = v[0] = v[1] = make_float2(0.f, 0.f);
+    at = 0;
   }
-  const float m = base_of(a.m);
+  __device__ __forceinline__ Sums sums() const {
+    return Sums{m, (s[0].x + s[0].y) + (s[1].x + s[1].y), (v[0].x + v[0].y) + (v[1].x + v[1].y)};
+  }
+  // K vectors (unavailable entries already at the floor); vector k starts at element i0 + k * step.
+  template <int K>
+  __device__ __forceinline__ void add(uint4 (&r)[K], int i0, int step, float c) {
+    float t[K];
 #pragma unroll
-  for (int j = 0; j < N; j += 2) add_values(a, v[j], v[j + 1], m, c);
-}
+    for (int k = 0; k < K; ++k) {
+      r[k].x = Vec<T>::raise(r[k].x);
+      r[k].y = Vec<T>::raise(r[k].y);
+      r[k].z = Vec<T>::raise(r[k].z);
+      r[k].w = Vec<T>::raise(r[k].w);
+      t[k] = Vec<T>::largest(r[k]);
+    }
+    float top = t[0];
+#pragma unroll
+    for (int k = 1; k < K; ++k) top = max_nan(top, t[k]);
+    if (!(top <= m)) {  // (also when top or m is NaN)
+#pragma unroll
+      for (int k = K - 1; k >= 0; --k)
+        if (!(t[k] < top)) at = i0 + k * step;
+      top = max_nan(m, top);
+      const float d = step_down(m, top, c), f = ex2(d);
+      const float2 f2 = make_float2(f, f), d2 = make_float2(d, d);
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        v[h] = mul2(f2, fma2(d2, s[h], v[h]));
+        s[h] = mul2(f2, s[h]);
+      }
+      m = top;
+    }
+    const float2 c2 = make_float2(c, c), m2 = make_float2(-m, -m);
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      float x[N];
+      Vec<T>::unpack(r[k], x);
+#pragma unroll
+      for (int j = 0; j < N; j += 2) {
+        const float2 u = mul2(add2(make_float2(x[j], x[j + 1]), m2), c2), e = make_float2(ex2(u.x), ex2(u.y));
+        s[j / 2 & 1] = add2(s[j / 2 & 1], e);
+        v[j / 2 & 1] = fma2(e, u, v[j / 2 & 1]);
+      }
+    }
+  }
+  __device__ __forceinline__ void add_one(float x, bool on, int i, float c) {  // one element a lane
+    x = on ? max_nan(x, Vec<T>::floor_value()) : Vec<T>::floor_value();
+    if (!(x <= m)) {
+      Sums a = sums();
+      rescale(a, max_nan(m, x), c);
+      m = a.m;
+      s[0] = make_float2(a.s, 0.f);
+      v[0] = make_float2(a.v, 0.f);
+      s[1] = v[1] = make_float2(0.f, 0.f);
+      at = i;
+    }
+    const float u = (x - m) * c, e = on ? ex2(u) : 0.f;
+    s[0].x += e;
+    v[0].x += e * u;
+  }
+};
 
 // ---- rows of more than SMALL_A actions ------------------------------------------------------------------------------
-// WARPS warps of a block walk a row together, 16 bytes a lane, each warp every WARPS-th group of 512 bytes; with WARPS = 1 a block holds
-// eight rows.  Few rows are divided over the blocks of a cluster in the same way.  A row that starts off a 16-byte boundary has up to 15
-// bytes in front and behind that the first and the last warp take element by element.
-// The alternatives cost the pass nothing: each lane knows the largest value that it has met, and the top-th largest of a block's such
-// values is met or exceeded by at least `top` entries of the row.  Behind the pass only the lanes whose largest value reaches
-// that bar are walked again, by their whole warp, from the cache.
-constexpr int WIDE_THREADS = 256;
+// A row that starts off a 16-byte boundary has up to 15 bytes in front of its vectors of 16 bytes and behind them, which are taken element by
+// element.
+template <typename T, bool MASK>
+struct Row {
+  static constexpr int N = Vec<T>::N;
+  const T* x;
+  const uint8_t* av;
+  int head, body, tail;  // elements, vectors, elements
+  __device__ __forceinline__ Row(const RowsParams& p, long long row) {
+    x = reinterpret_cast<const T*>(p.x) + row * p.xs;
+    av = MASK ? p.avail + row * p.as : nullptr;
+    const int off = (int)((16 - (reinterpret_cast<uintptr_t>(x) & 15)) & 15) / (int)sizeof(T);
+    head = off < p.A ? off : p.A;
+    body = (p.A - head) / N;
+    tail = p.A - head - body * N;
+  }
+  __device__ __forceinline__ const uint4* vectors() const { return reinterpret_cast<const uint4*>(x + head); }
+  // element i: its value, -infinity where it is not available
+  __device__ __forceinline__ float value(int i) const { return !MASK || av[i] ? to_f32(x[i]) : -INFINITY; }
+  // vector i with its unavailable entries at the floor
+  __device__ __forceinline__ uint4 vector(int i) const {
+    uint4 r = __ldg(vectors() + i);
+    if (MASK) {
+      uint32_t w[N / 4];
+      load_avail<N>(av + head + i * N, w);
+      Vec<T>::hide(r, w);
+    }
+    return r;
+  }
+  // vector i with its unavailable entries at -infinity
+  __device__ __forceinline__ void values(int i, float (&v)[N]) const {
+    Vec<T>::unpack(__ldg(vectors() + i), v);
+    if (MASK) {
+      uint32_t w[N / 4];
+      load_avail<N>(av + head + i * N, w);
+#pragma unroll
+      for (int j = 0; j < N; ++j)
+        if (!(w[j / 4] >> (8 * (j & 3)) & 0xFF)) v[j] = -INFINITY;
+    }
+  }
+};
 
-template <typename T, int WARPS, bool TOP, bool MASK>
-__global__ void __launch_bounds__(WIDE_THREADS) logprob_wide_kernel(const __grid_constant__ RowsParams p) {
-  constexpr int N = Vec<T>::N, ROWS = WIDE_THREADS / 32 / WARPS;
-  const int lane = threadIdx.x & 31, warp = (threadIdx.x >> 5) % WARPS, sub = (threadIdx.x >> 5) / WARPS;
-  const int parts = WARPS > 1 ? p.parts : 1, rank = WARPS > 1 ? (int)(blockIdx.x % parts) : 0;
-  const long long row = WARPS > 1 ? (long long)blockIdx.x / parts : (long long)blockIdx.x * ROWS + sub;
-  if (row >= p.rows) return;  // (WARPS = 1 only: no barrier follows)
-  const T* x = reinterpret_cast<const T*>(p.x) + row * p.xs;
-  const uint8_t* av = MASK ? p.avail + row * p.as : nullptr;
-  const int off = (int)((16 - (reinterpret_cast<uintptr_t>(x) & 15)) & 15) / (int)sizeof(T);
-  const int head = off < p.A ? off : p.A, body = (p.A - head) / N, tail = p.A - head - body * N;
-  const int stride = 32 * WARPS * parts, first = (rank * WARPS + warp) * 32;
-  const bool does_head = head && first == 0, does_tail = tail && rank == parts - 1 && warp == WARPS - 1;
+// This lane's share of a row: vectors first, first + stride, ..., K on their way at a time.
+template <int K, typename T, bool MASK>
+__device__ __forceinline__ void walk_vectors(Run<T>& run, const Row<T, MASK>& r, int first, int stride, float c) {
+  constexpr int N = Vec<T>::N;
+  int i = first;
+  if (i + (K - 1) * stride < r.body) {
+    uint4 next[K];
+#pragma unroll
+    for (int k = 0; k < K; ++k) next[k] = r.vector(i + k * stride);
+    for (;;) {
+      uint4 now[K];
+#pragma unroll
+      for (int k = 0; k < K; ++k) now[k] = next[k];
+      const int at = r.head + i * N;
+      i += K * stride;
+      const bool more = i + (K - 1) * stride < r.body;
+      if (more) {
+#pragma unroll
+        for (int k = 0; k < K; ++k) next[k] = r.vector(i + k * stride);
+      }
+      run.template add<K>(now, at, stride * N, c);
+      if (!more) break;
+    }
+  }
+  for (; i < r.body; i += stride) {
+    uint4 now[1] = {r.vector(i)};
+    run.template add<1>(now, r.head + i * N, 0, c);
+  }
+}
 
-  Sums2 a2{-INFINITY, make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
-  const uint4* xv = reinterpret_cast<const uint4*>(x + head);
-  auto load_one = [&](int i0, int n, float (&v)[N]) {  // n < N elements from i0 on, one a lane
-#pragma unroll
-    for (int j = 0; j < N; ++j) v[j] = -INFINITY;
-    if (lane < n && (!MASK || av[i0 + lane])) v[0] = to_f32(x[i0 + lane]);
-  };
-  auto hide = [&](int i, float (&v)[N]) {
-    uint32_t w[N / 4];
-    load_avail<N>(av + head + (long long)i * N, w);
-#pragma unroll
-    for (int j = 0; j < N; ++j)
-      if (!(w[j / 4] >> (8 * (j & 3)) & 0xFF)) v[j] = -INFINITY;
-  };
-  if (does_head) {
-    float v[N];
-    load_one(0, head, v);
-    add_values<N>(a2, v, p.c);
-  }
-  int i = first + lane;
-  for (; i + 3 * stride < body; i += 4 * stride) {  // four loads on their way at a time
-    uint4 r[4];
-#pragma unroll
-    for (int k = 0; k < 4; ++k) r[k] = __ldg(xv + i + k * stride);
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      float v[N];
-      Vec<T>::unpack(r[k], v);
-      if (MASK) hide(i + k * stride, v);
-      add_values<N>(a2, v, p.c);
-    }
-  }
-  for (; i < body; i += stride) {
-    float v[N];
-    Vec<T>::unpack(__ldg(xv + i), v);
-    if (MASK) hide(i, v);
-    add_values<N>(a2, v, p.c);
-  }
-  __syncwarp();
-  if (does_tail) {
-    float v[N];
-    load_one(head + body * N, tail, v);
-    add_values<N>(a2, v, p.c);
-  }
-
-  const float lane_max = a2.m;
-  Sums a{a2.m, a2.s.x + a2.s.y, a2.v.x + a2.v.y};
-  join_lanes(a, p.c);
-  __shared__ Sums part[WARPS];
-  __shared__ int keys[TOP && WARPS > 1 ? WARPS : 1][32];
-  __shared__ Entry lists[TOP && WARPS > 1 ? WARPS : 1][32];
-  const int mine_key = TOP ? order_key(lane_max) : 0;
-  int bar = TOP ? sort_keys(mine_key, lane) : 0;
-  if (WARPS > 1) {
-    if (lane == 0) part[warp] = a;
-    if (TOP) {
-#pragma unroll
-      for (int w = 1; w < WARPS; w *= 2) {  // pairs of warps, pairs of pairs ...
-        if (warp % (2 * w) == w) keys[warp][lane] = bar;
-        __syncthreads();
-        if (warp % (2 * w) == 0) bar = merge_keys(bar, keys[warp + w][31 - lane], lane);
-      }
-      if (warp == 0 && lane == p.top - 1) keys[0][0] = bar;
-    }
-    __syncthreads();
-    if (TOP) bar = keys[0][0];
-  } else if (TOP) bar = __shfl_sync(~0u, bar, p.top - 1);
-  Entry best = entry_none();
-  if (TOP) {
-    float v[N];
-    if (does_head) {
-      load_one(0, head, v);
-      take(best, v, lane, lane, p.top, bar);
-    }
-    // the walk of a lane is `steps` vectors, `stride` apart: as many lanes' as fit are read again at a time
-    unsigned who = __ballot_sync(~0u, mine_key >= bar && mine_key > KEY_NEG_INF);
-    const int steps = first < body ? (body - first + stride - 1) / stride : 0;
-    int lg = 0;
-    while ((1 << lg) < steps && lg < 5) ++lg;
-    while (who) {
-      unsigned m = who;
-      for (int k = lane >> lg; k && m; --k) m &= m - 1;
-      const int l = m ? __ffs(m) - 1 : 0;
-      for (int s0 = 0; s0 < steps; s0 += 1 << lg) {
-        const long long k = first + l + (long long)(s0 + (lane & ((1 << lg) - 1))) * stride;
-        if (m && k < body) {
-          Vec<T>::unpack(__ldg(xv + k), v);
-          if (MASK) hide((int)k, v);
-        } else {
-#pragma unroll
-          for (int j = 0; j < N; ++j) v[j] = -INFINITY;
-        }
-        take(best, v, head + (int)k * N, lane, p.top, bar);
-      }
-      for (int k = 32 >> lg; k && who; --k) who &= who - 1;
-    }
-    if (does_tail) {
-      load_one(head + body * N, tail, v);
-      take(best, v, head + body * N + lane, lane, p.top, bar);
-    }
-  }
-  if (WARPS > 1) {
-    if (TOP) lists[warp][lane] = best;
-    __syncthreads();
-    if (warp == 0) {
-#pragma unroll 1
-      for (int w = 1; w < WARPS; ++w) {
-        a = join(a, part[w], p.c);
-        if (TOP) merge_list(best, lists[w][lane], lane);
-      }
-    }
-    if (parts > 1) {  // the blocks' sums and lists, in the order of their ranks
-      cg::cluster_group cluster = cg::this_cluster();
-      if (warp == 0) {
-        if (lane == 0) part[0] = a;
-        if (TOP) lists[0][lane] = best;
-      }
-      cluster.sync();
-      if (rank == 0 && warp == 0) {
-        for (int r = 1; r < parts; ++r) {
-          a = join(a, *cluster.map_shared_rank(&part[0], r), p.c);
-          if (TOP) merge_list(best, *cluster.map_shared_rank(&lists[0][lane], r), lane);
+// Walks a warp's qualifying lanes again: lane l's vectors are first + l, first + l + stride, ...; as many lanes' as fit are read at a time.
+template <int CAP, typename T, bool MASK>
+__device__ __forceinline__ void rewalk(const Row<T, MASK>& r, int first, int stride, int lane, const Entry& mine, const Bar& bar, Entry* found,
+                                       int* count) {
+  constexpr int N = Vec<T>::N;
+  unsigned who = __ballot_sync(~0u, reaches(mine, bar.e));
+  const int steps = first < r.body ? (r.body - first + stride - 1) / stride : 0;
+  int lg = 0;
+  while ((1 << lg) < steps && lg < 5) ++lg;
+  while (who) {
+    unsigned m = who;
+    for (int k = lane >> lg; k && m; --k) m &= m - 1;
+    if (m)
+      for (int s = lane & ((1 << lg) - 1); s < steps; s += 1 << lg) {
+        const long long i = first + (__ffs(m) - 1) + (long long)s * stride;
+        if (i < r.body) {
+          float v[N];
+          r.values((int)i, v);
+          collect<N, CAP>(v, r.head + (int)i * N, bar, found, count);
         }
       }
-      cluster.sync();
-      if (rank) return;
-    }
-    if (warp) return;
+    for (int k = 32 >> lg; k && who; --k) who &= who - 1;
   }
+}
+
+// Elements in front of the vectors or behind them, one a lane, among the candidates.
+template <int N, int CAP>
+__device__ __forceinline__ void collect_one(float x, int i, const Bar& bar, Entry* found, int* count) {
+  if (x < bar.value || x == -INFINITY) return;
+  const Entry e{order_key(x), i};
+  if (e.key > bar.e.key || (e.key == bar.e.key && e.idx - N < bar.e.idx)) {
+    const int at = atomicAdd(count, 1);
+    if (at < CAP) found[at] = e;
+  }
+}
+
+// The results of a row, by one warp, from its joined sums and its list (lane k: the k-th alternative).
+template <bool TOP, bool MASK, typename T>
+__device__ __forceinline__ void write_results(const RowsParams& p, long long row, const Row<T, MASK>& r, Sums a, const Entry& best, int lane) {
+  if (!trusted(a, Vec<T>::floor_value(), p.c)) a = careful_sums<T>(r.x, r.av, p.A, p.c, lane);
+  float ls = 0.f;
   if (lane == 0) {
     const int act = p.action[row];
     const bool has = act >= 0 && act < p.A;
-    write_row(p, row, a, has, has && (!MASK || av[act]) ? to_f32(x[act]) : -INFINITY);
+    ls = write_row(p, row, a, has, has ? r.value(act) : -INFINITY);
   }
-  if (TOP && lane < p.top) {
-    const bool some = best.key > KEY_NEG_INF;
-    p.top_index[row * p.top + lane] = some ? best.idx : -1;
-    p.top_logp[row * p.top + lane] = some ? (to_f32(x[best.idx]) - a.m) * p.it - logf(a.s) : -INFINITY;
+  if (TOP) {
+    ls = __shfl_sync(~0u, ls, 0);
+    if (lane < p.top) {
+      const bool some = best.key > KEY_NEG_INF;
+      p.top_index[row * p.top + lane] = some ? best.idx : -1;
+      p.top_logp[row * p.top + lane] = some ? ((best.key == INT32_MAX ? NAN : key_value(best.key)) - a.m) * p.it - ls : -INFINITY;
+    }
   }
+}
+
+// -- a warp per row: eight rows a block.
+constexpr int WARP_ROWS = 8, WARP_CAP = 96;
+
+template <typename T, int K, bool TOP, bool MASK>
+__global__ void __launch_bounds__(WARP_ROWS * 32) logprob_warp_kernel(const __grid_constant__ RowsParams p) {
+  constexpr int N = Vec<T>::N;
+  __shared__ Entry found_all[TOP ? WARP_ROWS : 1][WARP_CAP];
+  __shared__ int count_all[WARP_ROWS];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const long long row = (long long)blockIdx.x * WARP_ROWS + warp;
+  if (row >= p.rows) return;
+  const Row<T, MASK> r(p, row);
+  const int back = r.head + r.body * N;
+  if (TOP && lane == 0) count_all[warp] = 0;
+  Run<T> run;
+  if (r.head) run.add_one(lane < r.head ? r.value(lane) : -INFINITY, lane < r.head, lane, p.c);
+  walk_vectors<K>(run, r, lane, 32, p.c);
+  if (r.tail) run.add_one(lane < r.tail ? r.value(back + lane) : -INFINITY, lane < r.tail, back + lane, p.c);
+  __syncwarp();
+  Sums a = run.sums();
+  join_lanes(a, p.c);
+  Entry best = entry_none();
+  if constexpr (TOP) {
+    Entry* found = found_all[warp];
+    int* count = &count_all[warp];
+    const Entry mine = lane_entry(run.m, run.at, Vec<T>::floor_value());
+    const Bar bar = make_bar(nth_best(mine, p.top, lane));
+    if (lane < r.head) collect_one<N, WARP_CAP>(r.value(lane), lane, bar, found, count);
+    rewalk<WARP_CAP>(r, 0, 32, lane, mine, bar, found, count);
+    if (lane < r.tail) collect_one<N, WARP_CAP>(r.value(back + lane), back + lane, bar, found, count);
+    __syncwarp();
+    const int n = *count;
+    if (n <= WARP_CAP) best = best_of(found, n, lane);
+    else walk<T>(best, r.x, r.av, 0, p.A, p.top, lane);
+  }
+  write_results<TOP>(p, row, r, a, best, lane);
+}
+
+// -- a block per row, or per part of a row (the parts are the blocks of a cluster).
+constexpr int BLOCK_WARPS = 4, BLOCK_THREADS = BLOCK_WARPS * 32, BLOCK_CAP = 512;
+
+template <typename T, bool TOP, bool MASK>
+__global__ void __launch_bounds__(BLOCK_THREADS) logprob_block_kernel(const __grid_constant__ RowsParams p) {
+  constexpr int N = Vec<T>::N;
+  __shared__ Sums part[BLOCK_WARPS];
+  __shared__ Entry marks[BLOCK_WARPS];
+  __shared__ Entry found[TOP ? BLOCK_CAP : 1];
+  __shared__ int count;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int parts = p.parts, rank = (int)(blockIdx.x % parts);
+  const long long row = blockIdx.x / parts;
+  const Row<T, MASK> r(p, row);
+  const int back = r.head + r.body * N, stride = BLOCK_THREADS * parts, first = rank * BLOCK_THREADS + warp * 32;
+  const int heads = rank == 0 && warp == 0 ? r.head : 0, tails = rank == parts - 1 && warp == BLOCK_WARPS - 1 ? r.tail : 0;
+  Run<T> run;
+  if (heads) run.add_one(lane < heads ? r.value(lane) : -INFINITY, lane < heads, lane, p.c);
+  walk_vectors<4>(run, r, first + lane, stride, p.c);
+  if (tails) run.add_one(lane < tails ? r.value(back + lane) : -INFINITY, lane < tails, back + lane, p.c);
+  __syncwarp();
+  Sums a = run.sums();
+  join_lanes(a, p.c);
+  const Entry mine = TOP ? lane_entry(run.m, run.at, Vec<T>::floor_value()) : entry_none();
+  // A bar that `top` lanes of the block reach: the best of the warps' top-th, or the worst of their best quarters of `top`, rounded up.
+  const bool few = p.top <= 2;
+  const Entry mark = TOP ? nth_best(mine, few ? p.top : (p.top + BLOCK_WARPS - 1) / BLOCK_WARPS, lane) : entry_none();
+  if (lane == 0) {
+    part[warp] = a;
+    marks[warp] = mark;
+    if (warp == 0) count = 0;
+  }
+  __syncthreads();
+  if constexpr (TOP) {
+    Entry e = marks[0];
+#pragma unroll
+    for (int w = 1; w < BLOCK_WARPS; ++w)
+      if (better(marks[w], e) == few) e = marks[w];
+    const Bar bar = make_bar(e);
+    if (lane < heads) collect_one<N, BLOCK_CAP>(r.value(lane), lane, bar, found, &count);
+    rewalk<BLOCK_CAP>(r, first, stride, lane, mine, bar, found, &count);
+    if (lane < tails) collect_one<N, BLOCK_CAP>(r.value(back + lane), back + lane, bar, found, &count);
+    __syncthreads();
+  }
+  Entry best = entry_none();
+  if (warp == 0) {
+    a = lane < BLOCK_WARPS ? part[lane] : Sums{Vec<T>::floor_value(), 0.f, 0.f};
+    join_lanes(a, p.c);
+    if constexpr (TOP) {
+      if (count <= BLOCK_CAP) best = best_of(found, count, lane);
+      else {
+        if (rank == 0) walk<T>(best, r.x, r.av, 0, r.head, p.top, lane);
+        for (int b = rank * BLOCK_THREADS; b < r.body; b += stride)
+          walk<T>(best, r.x, r.av, r.head + b * N, r.head + min(b + BLOCK_THREADS, r.body) * N, p.top, lane);
+        if (rank == parts - 1) walk<T>(best, r.x, r.av, back, p.A, p.top, lane);
+      }
+    }
+  }
+  if (parts > 1) {  // the blocks' sums and lists, in the order of their ranks
+    cg::cluster_group cluster = cg::this_cluster();
+    if (warp == 0) {
+      __syncwarp();
+      if (lane == 0) part[0] = a;
+      if (TOP) found[lane] = best;
+    }
+    cluster.sync();
+    if (rank == 0 && warp == 0) {
+      a = lane < parts ? *cluster.map_shared_rank(&part[0], lane < parts ? lane : 0) : Sums{Vec<T>::floor_value(), 0.f, 0.f};
+      join_lanes(a, p.c);
+      if (TOP)
+        for (int k = 1; k < parts; ++k) merge_list(best, *cluster.map_shared_rank(&found[lane], k), lane);
+    }
+    cluster.sync();
+    if (rank) return;
+  }
+  if (warp == 0) write_results<TOP>(p, row, r, a, best, lane);
 }
 
 // ---- rows of up to SMALL_A actions ----------------------------------------------------------------------------------
@@ -505,17 +723,33 @@ __global__ void __launch_bounds__(SMALL_ROWS) logprob_small_kernel(const __grid_
     v[j] = j < A ? mine[j] : -INFINITY;
     m = max_nan(m, v[j]);
   }
-  Sums2 a2{m, make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
-  const float b = base_of(m);
+  Sums a{m, 0.f, 0.f};
+  if (fabsf(m) < 1.0e30f) {
+    float2 s2 = make_float2(0.f, 0.f), v2 = s2;
+    const float2 c2 = make_float2(p.c, p.c), m2 = make_float2(-m, -m);
 #pragma unroll
-  for (int j = 0; j < MA; j += 2) add_values(a2, v[j], v[j + 1], b, p.c);
-  const Sums a{m, a2.s.x + a2.s.y, a2.v.x + a2.v.y};
+    for (int j = 0; j < MA; j += 2) {
+      float2 u = mul2(add2(make_float2(v[j], v[j + 1]), m2), c2);
+      u = make_float2(max_nan(u.x, -200.f), max_nan(u.y, -200.f));
+      const float2 e = make_float2(ex2(u.x), ex2(u.y));
+      s2 = add2(s2, e);
+      v2 = fma2(e, u, v2);
+    }
+    a.s = s2.x + s2.y;
+    a.v = v2.x + v2.y;
+  } else {  // empty rows, NaN, infinities, numbers whose differences may overflow
+    for (int j = 0; j < A; ++j) {
+      if (mine[j] == -INFINITY) continue;
+      const float u = exponent(mine[j], m, p.c), e = ex2(u);
+      a.s += e;
+      a.v += e * u;
+    }
+  }
   const long long row = row0 + r;
   const int act = p.action[row];
   const bool has = act >= 0 && act < A;
-  write_row(p, row, a, has, has ? mine[act] : -INFINITY);
+  const float ls = write_row(p, row, a, has, has ? mine[act] : -INFINITY);
   if (!p.top) return;
-  const float ls = logf(a.s);
   if (m != m) {  // a NaN ranks above all numbers: +infinity in its place, and that below it
 #pragma unroll
     for (int j = 0; j < MA; ++j) v[j] = v[j] != v[j] ? INFINITY : v[j] == INFINITY ? 3.402823466e38f : v[j];
@@ -761,6 +995,8 @@ static int launched(const char* what) {
   return e == cudaSuccess ? MARL_OK : fail(MARL_ECUDA, "%s: %s", what, cudaGetErrorString(e));
 }
 
+constexpr int WARP_A = 4096;  // the longest row that one warp walks
+
 // Rows without gaps, on boundaries that four elements and four bytes of availability need.
 template <typename T>
 static bool rows_dense(const RowsParams& p) {
@@ -782,31 +1018,38 @@ static int launch_logprob(const RowsParams& p, cudaStream_t stream) {
     else dense ? go(logprob_small_kernel<T, 32, true>) : go(logprob_small_kernel<T, 32, false>);
     return launched("marl_policy_logprob");
   }
-  const bool warp_rows = p.A <= 2048;
   RowsParams q = p;
   q.parts = 1;
-  if (!warp_rows)
-    while (q.parts < 8 && p.rows * q.parts * 2 <= 2 * LOGPROB_SMS && p.A / (q.parts * 2) >= 4096) q.parts *= 2;
-  const long long blocks = warp_rows ? (p.rows + 7) / 8 : p.rows * q.parts;
-  if (blocks > INT32_MAX) return fail(MARL_EINVAL, "too many rows");
   cudaLaunchConfig_t lc = {};
-  lc.gridDim = dim3((unsigned)blocks);
-  lc.blockDim = dim3(WIDE_THREADS);
-  lc.stream = stream;
   cudaLaunchAttribute at[1];
-  at[0].id = cudaLaunchAttributeClusterDimension;
-  at[0].val.clusterDim.x = (unsigned)q.parts;
-  at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
-  lc.attrs = at;
-  lc.numAttrs = q.parts > 1 ? 1 : 0;
+  lc.stream = stream;
+  long long blocks;
+  if (p.A <= WARP_A) {
+    blocks = (p.rows + WARP_ROWS - 1) / WARP_ROWS;
+    lc.blockDim = dim3(WARP_ROWS * 32);
+  } else {
+    while (q.parts < 8 && p.rows * q.parts * 2 <= 4 * LOGPROB_SMS && p.A / (q.parts * 2) >= 4096) q.parts *= 2;
+    blocks = p.rows * q.parts;
+    lc.blockDim = dim3(BLOCK_THREADS);
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.x = (unsigned)q.parts;
+    at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+    lc.attrs = at;
+    lc.numAttrs = q.parts > 1 ? 1 : 0;
+  }
+  if (blocks > INT32_MAX) return fail(MARL_EINVAL, "too many rows");
+  lc.gridDim = dim3((unsigned)blocks);
   cudaError_t err = cudaSuccess;
   auto go = [&](auto kernel) { err = cudaLaunchKernelEx(&lc, kernel, q); };
-  if (warp_rows) {
-    if (p.top) p.avail ? go(logprob_wide_kernel<T, 1, true, true>) : go(logprob_wide_kernel<T, 1, true, false>);
-    else p.avail ? go(logprob_wide_kernel<T, 1, false, true>) : go(logprob_wide_kernel<T, 1, false, false>);
+  if (p.A <= 32 * 4 * Vec<T>::N) {
+    if (p.top) p.avail ? go(logprob_warp_kernel<T, 1, true, true>) : go(logprob_warp_kernel<T, 1, true, false>);
+    else p.avail ? go(logprob_warp_kernel<T, 1, false, true>) : go(logprob_warp_kernel<T, 1, false, false>);
+  } else if (p.A <= WARP_A) {
+    if (p.top) p.avail ? go(logprob_warp_kernel<T, 4, true, true>) : go(logprob_warp_kernel<T, 4, true, false>);
+    else p.avail ? go(logprob_warp_kernel<T, 4, false, true>) : go(logprob_warp_kernel<T, 4, false, false>);
   } else {
-    if (p.top) p.avail ? go(logprob_wide_kernel<T, 8, true, true>) : go(logprob_wide_kernel<T, 8, true, false>);
-    else p.avail ? go(logprob_wide_kernel<T, 8, false, true>) : go(logprob_wide_kernel<T, 8, false, false>);
+    if (p.top) p.avail ? go(logprob_block_kernel<T, true, true>) : go(logprob_block_kernel<T, true, false>);
+    else p.avail ? go(logprob_block_kernel<T, false, true>) : go(logprob_block_kernel<T, false, false>);
   }
   if (err != cudaSuccess) return fail(MARL_ECUDA, "marl_policy_logprob: %s", cudaGetErrorString(err));
   return launched("marl_policy_logprob");

@@ -285,3 +285,26 @@ def test_refusals():
         binding.marl_policy_logprob_backward(x, act, r["stats"], r["entropy"], g_logp=torch.ones(3, device="cuda"))
     with pytest.raises(e):
         binding.marl_policy_logprob_backward(x, act, r["stats"], r["entropy"], out=x.half())
+
+
+@pytest.mark.parametrize("dt", ["fp32", "bf16"])
+@pytest.mark.parametrize("R,A,top", [(300, 4097, 8), (400, 9001, 1), (1200, 5000, 20), (297, 20011, 3)])
+@pytest.mark.parametrize("mask", [True, False])
+def test_many_long_rows(R, A, top, dt, mask):
+    x, av, act = _make(R, A, dt, R, mask, pad=R % 2)
+    _check(x, av, act, T=0.8, top=top)
+
+
+@pytest.mark.parametrize("R,A", [(3, 1500), (2, 40000), (310, 16385)])
+def test_large_values_in_few_lanes(R, A):
+    """Periods at which one lane of a warp, or of a block, meets nearly all large values: more candidates than there is room for."""
+    j = torch.arange(A)
+    rows = []
+    for period in (32 * 8, 256 * 8, 32 * 4, 512 * 8, 1024 * 8):
+        rows.append(torch.where(j % period < 8, 100.0 + (j * 37 % 101) / 64, -(j % 13) / 4.0))
+    v = torch.stack(rows)
+    for dt in ("fp32", "bf16"):
+        x = v.to(DT[dt]).cuda().repeat(-(-R // 5), 1)[:R].contiguous()
+        act = torch.zeros(R, dtype=torch.int32, device="cuda")
+        for top in (1, 5, 32):
+            _check(x, None, act, top=top, grads=False)
