@@ -200,9 +200,18 @@ __device__ __forceinline__ void collect(const float (&v)[N], int i0, const Bar& 
       }
     }
 }
-// The best 32 of n entries, one a lane, best first.
-__device__ __forceinline__ Entry best_of(const Entry* found, int n, int lane) {
+// The best `top` of n entries, one a lane, best first.
+__device__ __forceinline__ Entry best_of(const Entry* found, int n, int top, int lane) {
   Entry best = lane < n ? found[lane] : entry_none();
+  if (n <= 32 && top <= 8) {  // one by one
+    Entry out = entry_none();
+    for (int r = 0; r < top; ++r) {
+      const int key = __reduce_max_sync(~0u, best.key), idx = __reduce_min_sync(~0u, best.key == key ? best.idx : INT32_MAX);
+      if (best.idx == idx) best = entry_none();
+      if (lane == r) out = Entry{key, idx};
+    }
+    return out;
+  }
   sort_list(best, lane);
   for (int b = 32; b < n; b += 32) {
     Entry e = b + lane < n ? found[b + lane] : entry_none();
@@ -485,25 +494,24 @@ __device__ __forceinline__ void walk_vectors(Run<T>& run, const Row<T, MASK>& r,
 // Walks a warp's qualifying lanes again: lane l's vectors are first + l, first + l + stride, ...; as many lanes' as fit are read at a time.
 template <int CAP, typename T, bool MASK>
 __device__ __forceinline__ void rewalk(const Row<T, MASK>& r, int first, int stride, int lane, const Entry& mine, const Bar& bar, Entry* found,
-                                       int* count) {
+                                       int* count, uint8_t (&order)[32]) {
   constexpr int N = Vec<T>::N;
-  unsigned who = __ballot_sync(~0u, reaches(mine, bar.e));
-  const int steps = first < r.body ? (r.body - first + stride - 1) / stride : 0;
+  const unsigned who = __ballot_sync(~0u, reaches(mine, bar.e));
+  if (who >> lane & 1) order[__popc(who & ((1u << lane) - 1))] = (uint8_t)lane;
+  const int steps = first < r.body ? (r.body - first + stride - 1) / stride : 0, lanes = __popc(who);
   int lg = 0;
   while ((1 << lg) < steps && lg < 5) ++lg;
-  while (who) {
-    unsigned m = who;
-    for (int k = lane >> lg; k && m; --k) m &= m - 1;
-    if (m)
-      for (int s = lane & ((1 << lg) - 1); s < steps; s += 1 << lg) {
-        const long long i = first + (__ffs(m) - 1) + (long long)s * stride;
-        if (i < r.body) {
-          float v[N];
-          r.values((int)i, v);
-          collect<N, CAP>(v, r.head + (int)i * N, bar, found, count);
-        }
-      }
-    for (int k = 32 >> lg; k && who; --k) who &= who - 1;
+  __syncwarp();
+  for (int k = lane >> lg; k < lanes; k += 32 >> lg) {
+    const int l = first + order[k];
+    for (int s = lane & ((1 << lg) - 1); s < steps; s += 2 << lg) {  // two vectors on their way
+      const long long i = l + (long long)s * stride, i2 = i + ((long long)stride << lg);
+      float v[N], v2[N];
+      if (i < r.body) r.values((int)i, v);
+      if (i2 < r.body) r.values((int)i2, v2);
+      if (i < r.body) collect<N, CAP>(v, r.head + (int)i * N, bar, found, count);
+      if (i2 < r.body) collect<N, CAP>(v2, r.head + (int)i2 * N, bar, found, count);
+    }
   }
 }
 
@@ -546,6 +554,7 @@ __global__ void __launch_bounds__(WARP_ROWS * 32) logprob_warp_kernel(const __gr
   constexpr int N = Vec<T>::N;
   __shared__ Entry found_all[TOP ? WARP_ROWS : 1][WARP_CAP];
   __shared__ int count_all[WARP_ROWS];
+  __shared__ uint8_t order[WARP_ROWS][32];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const long long row = (long long)blockIdx.x * WARP_ROWS + warp;
   if (row >= p.rows) return;
@@ -566,24 +575,29 @@ __global__ void __launch_bounds__(WARP_ROWS * 32) logprob_warp_kernel(const __gr
     const Entry mine = lane_entry(run.m, run.at, Vec<T>::floor_value());
     const Bar bar = make_bar(nth_best(mine, p.top, lane));
     if (lane < r.head) collect_one<N, WARP_CAP>(r.value(lane), lane, bar, found, count);
-    rewalk<WARP_CAP>(r, 0, 32, lane, mine, bar, found, count);
+    rewalk<WARP_CAP>(r, 0, 32, lane, mine, bar, found, count, order[warp]);
     if (lane < r.tail) collect_one<N, WARP_CAP>(r.value(back + lane), back + lane, bar, found, count);
     __syncwarp();
     const int n = *count;
-    if (n <= WARP_CAP) best = best_of(found, n, lane);
+    if (n <= WARP_CAP) best = best_of(found, n, p.top, lane);
     else walk<T>(best, r.x, r.av, 0, p.A, p.top, lane);
   }
   write_results<TOP>(p, row, r, a, best, lane);
 }
 
 // -- a block per row, or per part of a row (the parts are the blocks of a cluster).
-constexpr int BLOCK_WARPS = 4, BLOCK_THREADS = BLOCK_WARPS * 32, BLOCK_CAP = 512;
+// Eight blocks an SM (64 registers a thread) and four vectors on their way while four are computed: 2048 rows of 65537 in bf16, none / one / eight
+// alternatives 50 / 57 / 72 us; with two vectors 58 / 65 / 79, with ten blocks and two vectors 60 / 67 / 83, twelve and one 82 / 88 / 106; with no
+// limit on the registers (five blocks) and four vectors 68 / 72 / 90.
+constexpr int EXACT_STEPS = 24;
+constexpr int BLOCK_THREADS = BLOCK_WARPS * 32, BLOCK_CAP = 512;
 
 template <typename T, bool TOP, bool MASK>
-__global__ void __launch_bounds__(BLOCK_THREADS) logprob_block_kernel(const __grid_constant__ RowsParams p) {
+__global__ void __launch_bounds__(BLOCK_THREADS, 8) logprob_block_kernel(const __grid_constant__ RowsParams p) {
   constexpr int N = Vec<T>::N;
   __shared__ Sums part[BLOCK_WARPS];
-  __shared__ Entry marks[BLOCK_WARPS];
+  __shared__ Entry marks[BLOCK_WARPS][32];
+  __shared__ uint8_t order[BLOCK_WARPS][32];
   __shared__ Entry found[TOP ? BLOCK_CAP : 1];
   __shared__ int count;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -600,23 +614,33 @@ __global__ void __launch_bounds__(BLOCK_THREADS) logprob_block_kernel(const __gr
   Sums a = run.sums();
   join_lanes(a, p.c);
   const Entry mine = TOP ? lane_entry(run.m, run.at, Vec<T>::floor_value()) : entry_none();
-  // A bar that `top` lanes of the block reach: the best of the warps' top-th, or the worst of their best quarters of `top`, rounded up.
-  const bool few = p.top <= 2;
-  const Entry mark = TOP ? nth_best(mine, few ? p.top : (p.top + BLOCK_WARPS - 1) / BLOCK_WARPS, lane) : entry_none();
+  // The bar: where a lane's walk is long, the top-th best of the block's lanes; where it is short, the worst of the warps' best
+  // quarters of `top`, which some half as many lanes more reach but which is sooner found.
+  const bool exact = p.top > 1 && (long long)stride * EXACT_STEPS < r.body;
+  Entry mark = mine;
+  if (TOP) {
+    if (exact) sort_list(mark, lane);
+    else mark = nth_best(mark, (p.top + BLOCK_WARPS - 1) / BLOCK_WARPS, lane);
+    marks[warp][lane] = mark;
+  }
   if (lane == 0) {
     part[warp] = a;
-    marks[warp] = mark;
     if (warp == 0) count = 0;
   }
   __syncthreads();
   if constexpr (TOP) {
-    Entry e = marks[0];
+    if (!exact) {
 #pragma unroll
-    for (int w = 1; w < BLOCK_WARPS; ++w)
-      if (better(marks[w], e) == few) e = marks[w];
-    const Bar bar = make_bar(e);
+      for (int w = 0; w < BLOCK_WARPS; ++w)
+        if (better(marks[w][0], mark) == (p.top == 1)) mark = marks[w][0];
+    } else {
+      for (int w = 0; w < BLOCK_WARPS; ++w)
+        if (w != warp) merge_list(mark, marks[w][lane], lane);
+      mark = shfl_entry(mark, p.top - 1);
+    }
+    const Bar bar = make_bar(mark);
     if (lane < heads) collect_one<N, BLOCK_CAP>(r.value(lane), lane, bar, found, &count);
-    rewalk<BLOCK_CAP>(r, first, stride, lane, mine, bar, found, &count);
+    rewalk<BLOCK_CAP>(r, first, stride, lane, mine, bar, found, &count, order[warp]);
     if (lane < tails) collect_one<N, BLOCK_CAP>(r.value(back + lane), back + lane, bar, found, &count);
     __syncthreads();
   }
@@ -625,7 +649,7 @@ __global__ void __launch_bounds__(BLOCK_THREADS) logprob_block_kernel(const __gr
     a = lane < BLOCK_WARPS ? part[lane] : Sums{Vec<T>::floor_value(), 0.f, 0.f};
     join_lanes(a, p.c);
     if constexpr (TOP) {
-      if (count <= BLOCK_CAP) best = best_of(found, count, lane);
+      if (count <= BLOCK_CAP) best = best_of(found, count, p.top, lane);
       else {
         if (rank == 0) walk<T>(best, r.x, r.av, 0, r.head, p.top, lane);
         for (int b = rank * BLOCK_THREADS; b < r.body; b += stride)
@@ -797,19 +821,20 @@ struct RowGrad {
   int action;             // -1: none
 };
 __device__ __forceinline__ RowGrad row_grad(const RowsGradParams& q, long long row) {
-  const float2 st = q.r.stats[row];
+  const float2 st = q.r.stats[row];  // (all loads at once)
+  const int act = q.r.action[row];
+  const float gl = q.g_logp ? q.g_logp[row] : 0.f, ge = q.g_entropy ? q.g_entropy[row] : 0.f, entropy = q.r.entropy[row];
   RowGrad r{0.f, 0.f, 0.f, 0.f, 0.f, -1};
   if (st.y == -INFINITY) return r;  // an empty row: nothing in it is available
-  const int act = q.r.action[row];
   if (act >= 0 && act < q.r.A) {
     r.action = act;
-    r.g = q.g_logp ? q.g_logp[row] * q.r.it : 0.f;
+    r.g = gl * q.r.it;
   }
-  const float h = q.g_entropy ? q.g_entropy[row] * q.r.it : 0.f;
+  const float h = ge * q.r.it;
   r.m = st.x;
   r.ls2 = st.y * LOG2E;
   r.h = h * LN2;
-  r.k = r.g + h * q.r.entropy[row];
+  r.k = r.g + h * entropy;
   return r;
 }
 // x of an available entry, or -infinity: 0 then.
@@ -829,30 +854,22 @@ __global__ void __launch_bounds__(256) logprob_wide_grad_kernel(const __grid_con
   const long long row = unit / q.segments;
   if (row >= q.r.rows) return;
   const int segment = (int)(unit - row * q.segments), A = q.r.A;
-  const RowGrad g = row_grad(q, row);
   const T* x = reinterpret_cast<const T*>(q.r.x) + row * q.r.xs;
   const uint8_t* av = MASK ? q.r.avail + row * q.r.as : nullptr;
   T* d = reinterpret_cast<T*>(q.dx) + row * q.ds;
   const float c = q.r.c;
   const int off = (int)((16 - (reinterpret_cast<uintptr_t>(d) & 15)) & 15) / (int)sizeof(T);
   const int head = off < A ? off : A, body = (A - head) / N, tail = A - head - body * N;
-  auto single = [&](int j) {
-    float v = to_f32(x[j]);
-    if (MASK && !av[j]) v = -INFINITY;
-    float o = entry_grad(g.m, g.ls2, g.k, g.h, v, c);
-    if (j == g.action && v != -INFINITY) o += g.g;
-    d[j] = from_f32<T>(o);
-  };
-  if (segment == 0 && lane < head) single(lane);
-  if (segment == q.segments - 1 && lane < tail) single(head + body * N + lane);
   const int i0 = segment * q.seg_len, i1 = min(body, i0 + q.seg_len);  // vectors
   const uintptr_t xa = reinterpret_cast<uintptr_t>(x + head);
   const uint4* xv = reinterpret_cast<const uint4*>(xa & ~(uintptr_t)15);
   const int shift = (int)(xa & 15);                                    // bytes
-  constexpr int BATCH = 4;  // vectors on their way at a time (the gradient may be written over the logits: no load moves up past a store)
-  for (int b = i0; b < i1; b += 32 * BATCH) {
-    uint4 raw[BATCH], next[BATCH];
-    uint32_t w[BATCH][N / 4];
+  // BATCH vectors are on their way while BATCH are computed.  (The gradient may be written over the logits: every lane then reads
+  // and writes its own vectors only, each before it is written.)
+  constexpr int BATCH = 2;
+  uint4 raw[BATCH], next[BATCH];
+  uint32_t w[BATCH][N / 4];
+  auto fetch = [&](int b) {
 #pragma unroll
     for (int k = 0; k < BATCH; ++k) {
       const int i = b + 32 * k + lane;
@@ -862,13 +879,36 @@ __global__ void __launch_bounds__(256) logprob_wide_grad_kernel(const __grid_con
       if (shift && (lane == 31 || i + 1 == i1)) next[k] = *(xv + i + 1);
       if (MASK) load_avail<N>(av + head + i * N, w[k]);
     }
+  };
+  fetch(i0);
+  const RowGrad g = row_grad(q, row);
+  auto single = [&](int j) {
+    float v = to_f32(x[j]);
+    if (MASK && !av[j]) v = -INFINITY;
+    float o = entry_grad(g.m, g.ls2, g.k, g.h, v, c);
+    if (j == g.action && v != -INFINITY) o += g.g;
+    d[j] = from_f32<T>(o);
+  };
+  if (segment == 0 && lane < head) single(lane);
+  if (segment == q.segments - 1 && lane < tail) single(head + body * N + lane);
+  for (int b = i0; b < i1; b += 32 * BATCH) {
+    uint4 now[BATCH], behind[BATCH];
+    uint32_t on[BATCH][N / 4];
+#pragma unroll
+    for (int k = 0; k < BATCH; ++k) {
+      now[k] = raw[k];
+      behind[k] = next[k];
+#pragma unroll
+      for (int e = 0; e < N / 4; ++e) on[k][e] = w[k][e];
+    }
+    if (b + 32 * BATCH < i1) fetch(b + 32 * BATCH);
 #pragma unroll
     for (int k = 0; k < BATCH; ++k) {
       const int i = b + 32 * k + lane;
-      uint4 r = raw[k];
+      uint4 r = now[k];
       if (shift) {
         uint4 n{__shfl_down_sync(~0u, r.x, 1), __shfl_down_sync(~0u, r.y, 1), __shfl_down_sync(~0u, r.z, 1), __shfl_down_sync(~0u, r.w, 1)};
-        if (lane == 31 || i + 1 == i1) n = next[k];
+        if (lane == 31 || i + 1 == i1) n = behind[k];
         uint32_t t[8] = {r.x, r.y, r.z, r.w, n.x, n.y, n.z, n.w};
         if (shift & 8) {
 #pragma unroll
@@ -888,7 +928,7 @@ __global__ void __launch_bounds__(256) logprob_wide_grad_kernel(const __grid_con
       if (MASK) {
 #pragma unroll
         for (int j = 0; j < N; ++j)
-          if (!(w[k][j / 4] >> (8 * (j & 3)) & 0xFF)) v[j] = -INFINITY;
+          if (!(on[k][j / 4] >> (8 * (j & 3)) & 0xFF)) v[j] = -INFINITY;
       }
 #pragma unroll
       for (int j = 0; j < N; ++j) o[j] = entry_grad(g.m, g.ls2, g.k, g.h, v[j], c);
@@ -995,6 +1035,7 @@ static int launched(const char* what) {
   return e == cudaSuccess ? MARL_OK : fail(MARL_ECUDA, "%s: %s", what, cudaGetErrorString(e));
 }
 
+constexpr long long SEG_WARPS = 4 * 40ll * LOGPROB_SMS;
 constexpr int WARP_A = 4096;  // the longest row that one warp walks
 
 // Rows without gaps, on boundaries that four elements and four bytes of availability need.
@@ -1066,8 +1107,11 @@ static int launch_logprob_grad(RowsGradParams q, cudaStream_t stream) {
     else logprob_small_grad_kernel<T, false><<<(unsigned)blocks, SMALL_ROWS, 0, stream>>>(q, inv);
     return launched("marl_policy_logprob_backward");
   }
-  q.seg_len = q.r.A > 32768 ? 1024 : 256;
-  q.segments = std::max(1, (q.r.A / Vec<T>::N + q.seg_len - 1) / q.seg_len);
+  // Vectors a warp: as many as leave the device some four warps a slot, 64 at least.
+  const long long vectors = q.r.A / Vec<T>::N;
+  q.seg_len = 1024;
+  while (q.seg_len > 64 && q.r.rows * ((vectors + q.seg_len - 1) / q.seg_len) < SEG_WARPS) q.seg_len /= 2;
+  q.segments = (int)std::max<long long>(1, (vectors + q.seg_len - 1) / q.seg_len);
   const long long units = q.r.rows * q.segments, blocks = (units + 7) / 8;
   if (blocks > INT32_MAX) return fail(MARL_EINVAL, "too many rows");
   if (q.r.avail) logprob_wide_grad_kernel<T, true><<<(unsigned)blocks, 256, 0, stream>>>(q);
