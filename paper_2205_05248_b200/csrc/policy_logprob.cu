@@ -590,7 +590,7 @@ __global__ void __launch_bounds__(WARP_ROWS * 32) logprob_warp_kernel(const __gr
 // alternatives 50 / 57 / 72 us; with two vectors 58 / 65 / 79, with ten blocks and two vectors 60 / 67 / 83, twelve and one 82 / 88 / 106; with no
 // limit on the registers (five blocks) and four vectors 68 / 72 / 90.
 constexpr int EXACT_STEPS = 24;
-constexpr int BLOCK_THREADS = BLOCK_WARPS * 32, BLOCK_CAP = 512;
+constexpr int BLOCK_WARPS = 4, BLOCK_THREADS = BLOCK_WARPS * 32, BLOCK_CAP = 512;
 
 template <typename T, bool TOP, bool MASK>
 __global__ void __launch_bounds__(BLOCK_THREADS, 8) logprob_block_kernel(const __grid_constant__ RowsParams p) {
