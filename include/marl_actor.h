@@ -457,7 +457,7 @@ int marl_linear_scan_query(const marl_scan_t* in, size_t* states_bytes, size_t* 
 
 /* y [B][L][C] of dtype: 0 at and behind the end of a sequence, where the inputs are not read.  last f32[B][C].  states
  * f32[B][ceil(L / MARL_SCAN_INTERVAL)][C], the state that enters every MARL_SCAN_INTERVAL-th step in scan order, for the gradient (those
- * behind a sequence's end are not written); NULL: not kept.  work: scratch of at least work_bytes as queried, 8-byte aligned, may be
+ * behind a sequence's end are not written); NULL: not kept.  work: scratch of at least work_bytes as queried, 16-byte aligned, may be
  * NULL if that is 0. */
 int marl_linear_scan(void* stream, const marl_scan_t* in, void* y, float* last, float* states, void* work, size_t work_bytes);
 

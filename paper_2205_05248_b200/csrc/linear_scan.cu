@@ -11,6 +11,7 @@
 #include "launch_util.cuh"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace marl {
 
@@ -35,6 +36,8 @@ struct ScanParams {
   float* dh0;
   int lg;          // log2 of the lanes along the channels
   int warps;       // warps along time
+  int pipe;        // tiles by asynchronous copies
+  int steps;       // steps a thread holds: 1 (calls of one step) or STEPS
   int units;       // units (sequence, group of channels) a block
   int groups;      // groups of channels a sequence
   int chunks, chunk_len, intervals;
@@ -72,11 +75,14 @@ __device__ __forceinline__ void put(__nv_bfloat16* at, const float (&f)[2]) {
 __device__ __forceinline__ void put(__half* at, const float (&f)[2]) { *reinterpret_cast<__half2*>(at) = __floats2half2_rn(f[0], f[1]); }
 __device__ __forceinline__ void put(float* at, const float (&f)[2]) {}  // (fp32 has one channel a lane)
 
-// z = 1 / (1 + e^-g) and 1 - z, each accurate where it is small.
+// z = 1 / (1 + e^-g) and 1 - z = e^-g z, each accurate where it is small; below g = -87 z stays at 2^-126.
 __device__ __forceinline__ void gate_pair(float g, float& z, float& rest) {
-  const float e = ex2(-fabsf(g) * 1.4426950408889634f), big = __fdividef(1.f, 1.f + e), small = e * big;
-  z = g >= 0.f ? big : small;
-  rest = g >= 0.f ? small : big;
+  float t, r;
+  asm("min.NaN.f32 %0, %1, 0f42FC0000;" : "=f"(t) : "f"(g * -1.4426950408889634f));  // at most 126
+  const float e = ex2(t);
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.f + e));
+  z = r;
+  rest = e * r;
 }
 
 // Where a thread stands: its unit, lane of channels and place along time.
@@ -112,28 +118,52 @@ __device__ __forceinline__ void unit_sync(const ScanParams& p, const Place& w) {
   else asm volatile("bar.sync %0, %1;" ::"r"(w.slot + 1), "r"(p.warps * 32) : "memory");
 }
 
-// The cuts in front of the thread's steps k0 .. k0 + STEPS - 1 (scan order), as bits.
+// The cuts in front of the thread's steps k0 .. k0 + S - 1 (scan order), as bits.  The flags of a warp's steps are read side by side, a
+// lane a flag, and each thread takes its own out of the votes.
+template <int S>
 __device__ __forceinline__ unsigned load_cuts(const ScanParams& p, const Place& w, int k0) {
-  unsigned bits = 0;
-  if (!p.done) return 0;
   const uint8_t* d = p.done + (long long)w.b * p.L;
-#pragma unroll
-  for (int s = 0; s < STEPS; ++s) {
-    const int k = k0 + s, at = p.reverse ? w.n - 1 - k : k - 1;  // done of the step before, or in reverse of this one
-    if (k < w.n && at >= 0 && d[at]) bits |= 1u << s;
+  const int warp_k0 = k0 - w.sub * S, flags = (32 >> p.lg) * S;
+  unsigned mine = 0;
+  for (int f = 0; f < flags; f += 32) {
+    const int k = warp_k0 + f + w.lane, at = p.reverse ? w.n - 1 - k : k - 1;  // done of the step before, or in reverse of this one
+    const unsigned votes = __ballot_sync(~0u, f + w.lane < flags && k < w.n && at >= 0 && d[at < 0 ? 0 : at]);
+    const int at_bit = w.sub * S - f;  // (S divides 32: a thread's flags lie in one word)
+    if (at_bit >= 0 && at_bit < 32) mine = votes >> at_bit & ((1u << S) - 1);
   }
-  return bits;
+  return mine;
 }
 
-template <typename T, int V>
+// The thread's steps of one array; 0 where there is no step or no channel.
+template <typename T, int V, int S>
 __device__ __forceinline__ void load_steps(const void* base, long long sb, long long st, int sc, const ScanParams& p, const Place& w, int k0,
-                                           Raw<T, V> (&r)[STEPS]) {
-  const T* at = reinterpret_cast<const T*>(base) + w.b * sb + w.c * sc;
+                                           Raw<T, V> (&r)[S]) {
+  const T* at = reinterpret_cast<const T*>(base) + w.b * sb + w.c * sc + (p.reverse ? w.n - 1 - k0 : k0) * st;
+  const long long step = p.reverse ? -st : st;
+  if (w.on && k0 + S <= w.n) {
 #pragma unroll
-  for (int s = 0; s < STEPS; ++s) {
-    const int k = k0 + s, t = p.reverse ? w.n - 1 - k : k;
-    if (w.on && k < w.n) r[s] = *reinterpret_cast<const Raw<T, V>*>(at + t * st);
-    else r[s] = Raw<T, V>{};
+    for (int s = 0; s < S; ++s) r[s] = *reinterpret_cast<const Raw<T, V>*>(at + s * step);
+  } else {
+#pragma unroll
+    for (int s = 0; s < S; ++s) {
+      r[s] = Raw<T, V>{};
+      if (w.on && k0 + s < w.n) r[s] = *reinterpret_cast<const Raw<T, V>*>(at + s * step);
+    }
+  }
+}
+
+template <typename T, int V, int S>
+__device__ __forceinline__ void store_steps(T* row, const ScanParams& p, const Place& w, int k0, int end, const float (&v)[S][V]) {
+  T* at = row + (long long)(p.reverse ? w.n - 1 - k0 : k0) * p.C;
+  const long long step = p.reverse ? -(long long)p.C : p.C;
+  if (!w.on) return;
+  if (k0 + S <= end) {
+#pragma unroll
+    for (int s = 0; s < S; ++s) put(at + s * step, v[s]);
+  } else {
+#pragma unroll
+    for (int s = 0; s < S; ++s)
+      if (k0 + s < end) put(at + s * step, v[s]);
   }
 }
 
@@ -154,11 +184,13 @@ __device__ __forceinline__ void step_ab(bool live, float g, float x, float& a, f
   }
 }
 
+template <bool CUT>
 __device__ __forceinline__ Map shfl_map_up(const Map& m, int d) {
-  return Map{__shfl_up_sync(~0u, m.a, d), __shfl_up_sync(~0u, m.h, d), (bool)__shfl_up_sync(~0u, (int)m.cut, d)};
+  return Map{__shfl_up_sync(~0u, m.a, d), __shfl_up_sync(~0u, m.h, d), CUT && (bool)__shfl_up_sync(~0u, (int)m.cut, d)};
 }
+template <bool CUT>
 __device__ __forceinline__ Map shfl_map_down(const Map& m, int d) {
-  return Map{__shfl_down_sync(~0u, m.a, d), __shfl_down_sync(~0u, m.h, d), (bool)__shfl_down_sync(~0u, (int)m.cut, d)};
+  return Map{__shfl_down_sync(~0u, m.a, d), __shfl_down_sync(~0u, m.h, d), CUT && (bool)__shfl_down_sync(~0u, (int)m.cut, d)};
 }
 
 struct ScanShared {
@@ -186,13 +218,14 @@ __device__ __forceinline__ void enter_chunk(const ScanParams& p, const Place& w,
 }
 
 // AGG: only the chunk's map is computed, for the launch behind this one.
-template <typename T, int V, bool BLEND, bool AGG>
-__global__ void __launch_bounds__(MAX_WARPS * 32) scan_kernel(const __grid_constant__ ScanParams p) {
+template <typename T, int V, int S, bool BLEND, bool CUT, bool AGG>
+__global__ void __launch_bounds__(MAX_WARPS * 32, 4) scan_kernel(const __grid_constant__ ScanParams p) {
   __shared__ ScanShared sh_all;
   Place w;
   if (!find_place<V>(p, w)) return;
-  const int subs = 32 >> p.lg, tile = p.warps * subs * STEPS, wslot = w.slot * p.warps;
+  const int subs = 32 >> p.lg, tile = p.warps * subs * S, wslot = w.slot * p.warps, ch = w.lane & ((1 << p.lg) - 1);
   const int first = blockIdx.y * p.chunk_len, end = min(w.n, first + p.chunk_len);  // steps of this block, in scan order
+  T* y = reinterpret_cast<T*>(p.y) + (long long)w.b * p.L * p.C + w.c;
   float carry[V];
   Map whole[V];
 #pragma unroll
@@ -201,64 +234,55 @@ __global__ void __launch_bounds__(MAX_WARPS * 32) scan_kernel(const __grid_const
     whole[v] = Map{1.f, 0.f, false};
   }
   if (!AGG && p.chunks > 1 && first < w.n) enter_chunk<V, false>(p, w, blockIdx.y, 0, carry);
-
-  Raw<T, V> rg[STEPS], rx[STEPS];
-  unsigned cuts = 0;
-  if (first < end) {
-    load_steps<T, V>(p.g, p.gb, p.gt, p.gc, p, w, first + w.q * STEPS, rg);
-    load_steps<T, V>(p.x, p.xb, p.xt, p.xc, p, w, first + w.q * STEPS, rx);
-    cuts = load_cuts(p, w, first + w.q * STEPS);
-  }
   int par = 0;
   for (int k0 = first; k0 < end; k0 += tile, par ^= 1) {
-    const int mine = k0 + w.q * STEPS;
-    float a[STEPS][V], b[STEPS][V];
-    const unsigned cut = cuts;
+    const int mine = k0 + w.q * S;
+    float a[S][V], b[S][V];
+    unsigned cut = 0;
+    {
+      Raw<T, V> rg[S], rx[S];
+      load_steps<T, V, S>(p.g, p.gb, p.gt, p.gc, p, w, mine, rg);
+      load_steps<T, V, S>(p.x, p.xb, p.xt, p.xc, p, w, mine, rx);
+      if (CUT) cut = load_cuts<S>(p, w, mine);
 #pragma unroll
-    for (int s = 0; s < STEPS; ++s) {
-      float g[V], x[V];
-      unpack(rg[s], g);
-      unpack(rx[s], x);
+      for (int s = 0; s < S; ++s) {
+        float g[V], x[V];
+        unpack(rg[s], g);
+        unpack(rx[s], x);
 #pragma unroll
-      for (int v = 0; v < V; ++v) step_ab<BLEND>(mine + s < end, g[v], x[v], a[s][v], b[s][v]);
-    }
-    if (k0 + tile < end) {  // the next tile is on its way while this one is computed
-      load_steps<T, V>(p.g, p.gb, p.gt, p.gc, p, w, mine + tile, rg);
-      load_steps<T, V>(p.x, p.xb, p.xt, p.xc, p, w, mine + tile, rx);
-      cuts = load_cuts(p, w, mine + tile);
+        for (int v = 0; v < V; ++v) step_ab<BLEND>(mine + s < end, g[v], x[v], a[s][v], b[s][v]);
+      }
     }
     Map m[V], before[V];
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-      m[v] = Map{1.f, 0.f, cut != 0};
+      m[v] = Map{a[0][v], b[0][v], CUT && cut != 0};
 #pragma unroll
-      for (int s = 0; s < STEPS; ++s) {
-        m[v].h = cut >> s & 1 ? b[s][v] : fmaf(a[s][v], m[v].h, b[s][v]);
+      for (int s = 1; s < S; ++s) {
+        m[v].h = CUT && (cut >> s & 1) ? b[s][v] : fmaf(a[s][v], m[v].h, b[s][v]);
         m[v].a *= a[s][v];
-      }
-      for (int d = 1; d < subs; d <<= 1) {
-        const Map o = shfl_map_up(m[v], d << p.lg);
-        if (w.sub >= d) m[v] = then(o, m[v]);
       }
       before[v] = Map{1.f, 0.f, false};
       if (subs > 1) {
-        const Map o = shfl_map_up(m[v], 1 << p.lg);
+        for (int d = 1; d < subs; d <<= 1) {
+          const Map o = shfl_map_up<CUT>(m[v], d << p.lg);
+          if (w.sub >= d) m[v] = then(o, m[v]);
+        }
+        const Map o = shfl_map_up<CUT>(m[v], 1 << p.lg);
         if (w.sub) before[v] = o;
       }
     }
     float enter[V];
     if (p.warps > 1) {
       if (w.sub == subs - 1) {
-        const int ch = w.lane & ((1 << p.lg) - 1);
 #pragma unroll
         for (int v = 0; v < V; ++v) sh_all.total[par][wslot + w.warp][ch * V + v] = make_float2(m[v].a, m[v].h);
-        if (ch == 0) sh_all.cut[par][wslot + w.warp] = m[0].cut;
+        if (CUT && ch == 0) sh_all.cut[par][wslot + w.warp] = m[0].cut;
       }
       unit_sync(p, w);
-      const int ch = w.lane & ((1 << p.lg) - 1);
 #pragma unroll 4
       for (int i = 0; i < p.warps; ++i) {
-        const bool c = sh_all.cut[par][wslot + i];
+        const bool c = CUT && sh_all.cut[par][wslot + i];
 #pragma unroll
         for (int v = 0; v < V; ++v) {
           if (i == w.warp) enter[v] = carry[v];
@@ -274,7 +298,7 @@ __global__ void __launch_bounds__(MAX_WARPS * 32) scan_kernel(const __grid_const
         enter[v] = carry[v];
         Map t = m[v];
         if (subs > 1) {
-          const int src = 32 - (1 << p.lg) + (w.lane & ((1 << p.lg) - 1));
+          const int src = 32 - (1 << p.lg) + ch;
           t = Map{__shfl_sync(~0u, t.a, src), __shfl_sync(~0u, t.h, src), (bool)__shfl_sync(~0u, (int)t.cut, src)};
         }
         carry[v] = apply(t, carry[v]);
@@ -289,17 +313,14 @@ __global__ void __launch_bounds__(MAX_WARPS * 32) scan_kernel(const __grid_const
 #pragma unroll
         for (int v = 0; v < V; ++v) p.states[((long long)w.b * p.intervals + mine / MARL_SCAN_INTERVAL) * p.C + w.c + v] = h[v];
       }
-      T* y = reinterpret_cast<T*>(p.y) + (long long)w.b * p.L * p.C + w.c;
 #pragma unroll
-      for (int s = 0; s < STEPS; ++s) {
-        const int k = mine + s, t = p.reverse ? w.n - 1 - k : k;
+      for (int s = 0; s < S; ++s)
 #pragma unroll
-        for (int v = 0; v < V; ++v) h[v] = cut >> s & 1 ? b[s][v] : fmaf(a[s][v], h[v], b[s][v]);
-        if (w.on && k < end) put(y + (long long)t * p.C, h);
-      }
+        for (int v = 0; v < V; ++v) h[v] = a[s][v] = CUT && (cut >> s & 1) ? b[s][v] : fmaf(a[s][v], h[v], b[s][v]);
+      store_steps<T, V, S>(y, p, w, mine, end, a);
     }
   }
-  if (AGG) {
+  if constexpr (AGG) {
     if (first < end && w.q == 0) {
       if (w.on) {
 #pragma unroll
@@ -312,27 +333,26 @@ __global__ void __launch_bounds__(MAX_WARPS * 32) scan_kernel(const __grid_const
   }
   if (!w.on) return;
   if (w.q == 0 && (w.n > 0 ? end == w.n && first < w.n : blockIdx.y == 0)) {
-    const bool gone = !p.reverse && w.n > 0 && p.done && p.done[(long long)w.b * p.L + w.n - 1];
+    const bool gone = CUT && !p.reverse && w.n > 0 && p.done[(long long)w.b * p.L + w.n - 1];
 #pragma unroll
     for (int v = 0; v < V; ++v) p.last[(long long)w.b * p.C + w.c + v] = gone ? 0.f : carry[v];
   }
-  T* y = reinterpret_cast<T*>(p.y) + (long long)w.b * p.L * p.C + w.c;
   const float zero[V] = {};
   const int stop = min(p.L, first + p.chunk_len);
   for (int t = max(w.n, first) + w.q; t < stop; t += p.warps * subs) put(y + (long long)t * p.C, zero);
 }
 
-template <typename T, int V, bool BLEND, bool AGG>
-__global__ void __launch_bounds__(MAX_WARPS * 32) scan_grad_kernel(const __grid_constant__ ScanParams p) {
+template <typename T, int V, int S, bool BLEND, bool CUT, bool AGG>
+__global__ void __launch_bounds__(MAX_WARPS * 32, 2) scan_grad_kernel(const __grid_constant__ ScanParams p) {
   __shared__ ScanShared sh_all;
   Place w;
   if (!find_place<V>(p, w)) return;
-  const int subs = 32 >> p.lg, tile = p.warps * subs * STEPS, wslot = w.slot * p.warps, ch = w.lane & ((1 << p.lg) - 1);
+  const int subs = 32 >> p.lg, tile = p.warps * subs * S, wslot = w.slot * p.warps, ch = w.lane & ((1 << p.lg) - 1);
   const int first = blockIdx.y * p.chunk_len, end = min(w.n, first + p.chunk_len);
   const int used = (w.n + p.chunk_len - 1) / p.chunk_len;
   float carry[V];
   Map whole[V];
-  const bool gone = !p.reverse && w.n > 0 && p.done && p.done[(long long)w.b * p.L + w.n - 1];
+  const bool gone = CUT && !p.reverse && w.n > 0 && p.done[(long long)w.b * p.L + w.n - 1];
 #pragma unroll
   for (int v = 0; v < V; ++v) {
     carry[v] = !AGG && w.on && p.dlast && !gone ? p.dlast[(long long)w.b * p.C + w.c + v] : 0.f;
@@ -344,56 +364,47 @@ __global__ void __launch_bounds__(MAX_WARPS * 32) scan_grad_kernel(const __grid_
   const int tiles = first < end ? (end - first + tile - 1) / tile : 0;
   int par = 0;
   for (int i = tiles - 1; i >= 0; --i, par ^= 1) {
-    const int k0 = first + i * tile, mine = k0 + w.q * STEPS;
-    Raw<T, V> rg[STEPS], rx[STEPS], rd[STEPS];
-    load_steps<T, V>(p.g, p.gb, p.gt, p.gc, p, w, mine, rg);
-    load_steps<T, V>(p.dy, p.dyb, p.dyt, 1, p, w, mine, rd);
-    if (!AGG) load_steps<T, V>(p.x, p.xb, p.xt, p.xc, p, w, mine, rx);
-    const unsigned cut = load_cuts(p, w, mine);
-    float enter[V];
+    const int k0 = first + i * tile, mine = k0 + w.q * S;
+    // a: gate, q: 1 - gate (BLEND), x, d: gradient of y
+    float a[S][V], q[BLEND ? S : 1][V], x[S][V], d[S][V], enter[V];
+    unsigned cut = 0;
+    {
+      Raw<T, V> rg[S], rd[S], rx[S];
+      load_steps<T, V, S>(p.g, p.gb, p.gt, p.gc, p, w, mine, rg);
+      load_steps<T, V, S>(p.dy, p.dyb, p.dyt, 1, p, w, mine, rd);
+      if (!AGG) load_steps<T, V, S>(p.x, p.xb, p.xt, p.xc, p, w, mine, rx);
+      if (CUT) cut = load_cuts<S>(p, w, mine);
 #pragma unroll
-    for (int v = 0; v < V; ++v)
-      enter[v] = !AGG && w.on ? p.states[((long long)w.b * p.intervals + k0 / MARL_SCAN_INTERVAL) * p.C + w.c + v] : 0.f;
-    float a[STEPS][V], x[STEPS][V], d[STEPS][V];
-    Map m[V], r[V];   // the steps' map of the state, and that of the gradient (same factor, against the scan order)
+      for (int v = 0; v < V; ++v)
+        enter[v] = !AGG && w.on ? p.states[((long long)w.b * p.intervals + k0 / MARL_SCAN_INTERVAL) * p.C + w.c + v] : 0.f;
 #pragma unroll
-    for (int s = 0; s < STEPS; ++s) {
-      float g[V];
-      unpack(rg[s], g);
-      unpack(rd[s], d[s]);
-      if (!AGG) unpack(rx[s], x[s]);
+      for (int s = 0; s < S; ++s) {
+        unpack(rg[s], a[s]);
+        unpack(rd[s], d[s]);
+        if (!AGG) unpack(rx[s], x[s]);
 #pragma unroll
-      for (int v = 0; v < V; ++v) {
-        if (BLEND) {
-          float rest;
-          gate_pair(g[v], a[s][v], rest);
-        } else a[s][v] = g[v];
-        if (mine + s >= end) a[s][v] = 1.f;  // (x and dy are 0 there)
+        for (int v = 0; v < V; ++v) {
+          if (BLEND) gate_pair(a[s][v], a[s][v], q[s][v]);
+          if (mine + s >= end) a[s][v] = 1.f;  // (x and dy are 0 there)
+        }
       }
     }
-    // BLEND: the input of a step is (1 - z) x; 1 - z is computed again from the gate where it is needed
-    auto input = [&](int s, int v) {
-      if (!BLEND) return x[s][v];
-      float g[V], z, rest;
-      unpack(rg[s], g);
-      gate_pair(g[v], z, rest);
-      return mine + s < end ? rest * x[s][v] : 0.f;
-    };
+    Map m[V], r[V];   // the steps' map of the state, and that of the gradient (same factor, against the scan order)
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-      m[v] = r[v] = Map{1.f, 0.f, cut != 0};
+      m[v] = r[v] = Map{a[0][v], 0.f, CUT && cut != 0};
 #pragma unroll
-      for (int s = 0; s < STEPS; ++s) m[v].a *= a[s][v];
+      for (int s = 1; s < S; ++s) m[v].a *= a[s][v];
       r[v].a = m[v].a;
       if (!AGG) {
 #pragma unroll
-        for (int s = 0; s < STEPS; ++s) {
-          const float b = input(s, v);
-          m[v].h = cut >> s & 1 ? b : fmaf(a[s][v], m[v].h, b);
+        for (int s = 0; s < S; ++s) {
+          const float b = BLEND ? q[s][v] * x[s][v] : x[s][v];
+          m[v].h = CUT && (cut >> s & 1) ? b : fmaf(a[s][v], m[v].h, b);
         }
       }
 #pragma unroll
-      for (int s = STEPS - 1; s >= 0; --s) r[v].h = cut >> s & 1 ? 0.f : a[s][v] * (d[s][v] + r[v].h);
+      for (int s = S - 1; s >= 0; --s) r[v].h = CUT && (cut >> s & 1) ? 0.f : a[s][v] * (d[s][v] + r[v].h);
     }
     Map before[V], behind[V];
 #pragma unroll
@@ -401,13 +412,13 @@ __global__ void __launch_bounds__(MAX_WARPS * 32) scan_grad_kernel(const __grid_
       before[v] = behind[v] = Map{1.f, 0.f, false};
       if (subs > 1) {
         for (int e = 1; e < subs; e <<= 1) {
-          const Map o = shfl_map_up(m[v], e << p.lg), q = shfl_map_down(r[v], e << p.lg);
+          const Map o = shfl_map_up<CUT>(m[v], e << p.lg), t = shfl_map_down<CUT>(r[v], e << p.lg);
           if (w.sub >= e) m[v] = then(o, m[v]);
-          if (w.sub + e < subs) r[v] = then(q, r[v]);
+          if (w.sub + e < subs) r[v] = then(t, r[v]);
         }
-        const Map o = shfl_map_up(m[v], 1 << p.lg), q = shfl_map_down(r[v], 1 << p.lg);
+        const Map o = shfl_map_up<CUT>(m[v], 1 << p.lg), t = shfl_map_down<CUT>(r[v], 1 << p.lg);
         if (w.sub) before[v] = o;
-        if (w.sub + 1 < subs) behind[v] = q;
+        if (w.sub + 1 < subs) behind[v] = t;
         // the warp's maps: of the state in the last sub, of the gradient in the first
         const int last = 32 - (1 << p.lg) + ch;
         m[v] = Map{__shfl_sync(~0u, m[v].a, last), __shfl_sync(~0u, m[v].h, last), (bool)__shfl_sync(~0u, (int)m[v].cut, last)};
@@ -424,21 +435,23 @@ __global__ void __launch_bounds__(MAX_WARPS * 32) scan_grad_kernel(const __grid_
           sh_all.total[par][wslot + w.warp][ch * V + v] = make_float2(m[v].a, m[v].h);
           sh_all.back[par][wslot + w.warp][ch * V + v] = r[v].h;
         }
-        if (ch == 0) sh_all.cut[par][wslot + w.warp] = m[0].cut;
+        if (CUT && ch == 0) sh_all.cut[par][wslot + w.warp] = m[0].cut;
       }
       unit_sync(p, w);
+      if (!AGG)
+        for (int j = 0; j < w.warp; ++j)
+#pragma unroll
+          for (int v = 0; v < V; ++v) {
+            const float2 t = sh_all.total[par][wslot + j][ch * V + v];
+            enter[v] = apply(Map{t.x, t.y, CUT && sh_all.cut[par][wslot + j]}, enter[v]);
+          }
 #pragma unroll 4
-      for (int j = 0; j < p.warps; ++j) {
-        const int jb = p.warps - 1 - j;
-        const bool c = sh_all.cut[par][wslot + j], cb = sh_all.cut[par][wslot + jb];
+      for (int j = p.warps - 1; j >= 0; --j) {
+        const bool c = CUT && sh_all.cut[par][wslot + j];
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-          if (!AGG && j < w.warp) {
-            const float2 t = sh_all.total[par][wslot + j][ch * V + v];
-            enter[v] = apply(Map{t.x, t.y, c}, enter[v]);
-          }
-          if (jb == w.warp) back[v] = carry[v];
-          const Map mb{sh_all.total[par][wslot + jb][ch * V + v].x, sh_all.back[par][wslot + jb][ch * V + v], cb};
+          if (j == w.warp) back[v] = carry[v];
+          const Map mb{sh_all.total[par][wslot + j][ch * V + v].x, sh_all.back[par][wslot + j][ch * V + v], c};
           carry[v] = apply(mb, carry[v]);
           if (AGG) whole[v] = then(whole[v], mb);
         }
@@ -454,47 +467,33 @@ __global__ void __launch_bounds__(MAX_WARPS * 32) scan_grad_kernel(const __grid_
     if constexpr (!AGG) {
 #pragma unroll
       for (int v = 0; v < V; ++v) {
-        enter[v] = apply(before[v], enter[v]);
-        back[v] = apply(behind[v], back[v]);
-      }
-      float came[STEPS][V];  // the state that a step's gate multiplies
+        float h = apply(before[v], enter[v]), R = apply(behind[v], back[v]);
+        // d becomes G, then x and d become what is stored: (came - x) z (1 - z) G or came G, and (1 - z) G or G
 #pragma unroll
-      for (int v = 0; v < V; ++v) {
-        float h = enter[v];
-#pragma unroll
-        for (int s = 0; s < STEPS; ++s) {
-          if (cut >> s & 1) h = 0.f;
-          came[s][v] = h;
-          h = fmaf(a[s][v], h, input(s, v));
+        for (int s = S - 1; s >= 0; --s) {
+          d[s][v] += R;
+          R = CUT && (cut >> s & 1) ? 0.f : a[s][v] * d[s][v];
         }
-      }
 #pragma unroll
-      for (int s = STEPS - 1; s >= 0; --s) {
-        const int k = mine + s, t = p.reverse ? w.n - 1 - k : k;
-        float og[V], ox[V];
-#pragma unroll
-        for (int v = 0; v < V; ++v) {
-          const float G = d[s][v] + back[v];
+        for (int s = 0; s < S; ++s) {
+          if (CUT && (cut >> s & 1)) h = 0.f;
           if (BLEND) {
-            float g[V], z, rest;
-            unpack(rg[s], g);
-            gate_pair(g[v], z, rest);
-            og[v] = G * (came[s][v] - x[s][v]) * (z * rest);
-            ox[v] = G * rest;
+            const float G = d[s][v], b = q[s][v] * x[s][v];
+            d[s][v] = G * q[s][v];
+            x[s][v] = (h - x[s][v]) * (a[s][v] * d[s][v]);
+            h = fmaf(a[s][v], h, b);
           } else {
-            og[v] = G * came[s][v];
-            ox[v] = G;
+            const float b = x[s][v];
+            x[s][v] = d[s][v] * h;
+            h = fmaf(a[s][v], h, b);
           }
-          back[v] = cut >> s & 1 ? 0.f : a[s][v] * G;
-        }
-        if (w.on && k < end) {
-          put(dg + (long long)t * p.C, og);
-          put(dx + (long long)t * p.C, ox);
         }
       }
+      store_steps<T, V, S>(dg, p, w, mine, end, x);
+      store_steps<T, V, S>(dx, p, w, mine, end, d);
     }
   }
-  if (AGG) {
+  if constexpr (AGG) {
     if (first < end && w.q == 0) {
       if (w.on) {
 #pragma unroll
@@ -518,20 +517,392 @@ __global__ void __launch_bounds__(MAX_WARPS * 32) scan_grad_kernel(const __grid_
   }
 }
 
+// ---- aligned rows of many channels: tiles by asynchronous copies ----------------------------------------------------
+// A block takes 64 channels of a sequence, two a lane, in tiles of 64 steps, eight steps a warp.  The tiles of gate, x (and dy) come in
+// 16 bytes a copy into a ring of slots in shared memory, ahead of the tile that is computed; the arithmetic is packed, two channels
+// an operation.  The gradient reads x and dy from the slot twice rather than holding them.
+constexpr int PIPE_STEPS = 64, PIPE_CHANNELS = 64, PIPE_THREADS = 256, PIPE_WARPS = 8, PIPE_S = PIPE_STEPS / PIPE_WARPS;
+template <typename T> constexpr int PIPE_SLOTS = sizeof(T) == 4 ? 2 : 3;
+template <typename T, int ARRAYS> constexpr int SLOT_BYTES = ARRAYS * PIPE_STEPS * PIPE_CHANNELS * (int)sizeof(T);
+
+__device__ __forceinline__ float2 pair_of(const float* at) { return *reinterpret_cast<const float2*>(at); }
+__device__ __forceinline__ float2 pair_of(const __nv_bfloat16* at) { return __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(at)); }
+__device__ __forceinline__ float2 pair_of(const __half* at) { return __half22float2(*reinterpret_cast<const __half2*>(at)); }
+__device__ __forceinline__ void put_pair(float* at, float2 v) { *reinterpret_cast<float2*>(at) = v; }
+__device__ __forceinline__ void put_pair(__nv_bfloat16* at, float2 v) { *reinterpret_cast<__nv_bfloat162*>(at) = __floats2bfloat162_rn(v.x, v.y); }
+__device__ __forceinline__ void put_pair(__half* at, float2 v) { *reinterpret_cast<__half2*>(at) = __floats2half2_rn(v.x, v.y); }
+
+__device__ __forceinline__ void gate_pair2(float2 g, float2& z, float2& rest) {
+  const float2 t = mul2(g, make_float2(-1.4426950408889634f, -1.4426950408889634f));
+  float2 e, r;
+  asm("min.NaN.f32 %0, %1, 0f42FC0000;" : "=f"(e.x) : "f"(t.x));
+  asm("min.NaN.f32 %0, %1, 0f42FC0000;" : "=f"(e.y) : "f"(t.y));
+  e = make_float2(ex2(e.x), ex2(e.y));
+  const float2 u = add2(e, make_float2(1.f, 1.f));
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r.x) : "f"(u.x));
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r.y) : "f"(u.y));
+  z = r;
+  rest = mul2(e, r);
+}
+
+struct PipeShared {
+  float4 total[2][PIPE_WARPS][32];  // gate product and result of a warp's steps, two channels
+  float2 back[2][PIPE_WARPS][32];
+  __align__(8) uint8_t cut[2][PIPE_WARPS];
+};
+
+// What a block copies: row `k` (scan order) of an array at base + t stride, its 64 channels from chan0 on.
+template <typename T>
+struct Source {
+  const T* base;
+  long long stride;
+};
+template <typename T, int ARRAYS>
+__device__ __forceinline__ void copy_tile(const Source<T> (&src)[ARRAYS], const ScanParams& p, int n, int chan0, int k0, int end, uint8_t* slot) {
+  constexpr int PER = 16 / (int)sizeof(T), COPIES = PIPE_CHANNELS / PER, ROUNDS = PIPE_STEPS * COPIES / PIPE_THREADS;
+  if (k0 >= end) return;
+#pragma unroll
+  for (int j = 0; j < ROUNDS; ++j) {
+    const int i = threadIdx.x + j * PIPE_THREADS, row = i / COPIES, c = i % COPIES * PER, k = k0 + row;
+    if (k < end && chan0 + c < p.C) {
+      const int t = p.reverse ? n - 1 - k : k;
+#pragma unroll
+      for (int a = 0; a < ARRAYS; ++a) {
+        const uint32_t dst = (uint32_t)__cvta_generic_to_shared(slot + ((a * PIPE_STEPS + row) * PIPE_CHANNELS + c) * sizeof(T));
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src[a].base + t * src[a].stride + c) : "memory");
+      }
+    }
+  }
+}
+
+// The flag in front of step k0 + (lane & 7) of the warp's eight steps, as loaded; vote over the lanes 0 .. 7 to use it.
+__device__ __forceinline__ bool load_flag(const ScanParams& p, const uint8_t* done, int n, int k0, int lane) {
+  const int k = k0 + lane, at = p.reverse ? n - 1 - k : k - 1;
+  return lane < PIPE_S && k < n && at >= 0 && done[at] != 0;
+}
+
+__device__ __forceinline__ float2 apply2(float2 a, float2 h, bool cut, float2 in) { return cut ? h : fma2(a, in, h); }
+
+template <typename T, bool BLEND, bool CUT, bool AGG>
+__global__ void __launch_bounds__(PIPE_THREADS, 3) scan_pipe_kernel(const __grid_constant__ ScanParams p) {
+  constexpr int SLOTS = PIPE_SLOTS<T>;
+  extern __shared__ __align__(16) uint8_t slots[];
+  __shared__ PipeShared sh;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int b = blockIdx.x / p.groups, group = blockIdx.x % p.groups, chan0 = group * PIPE_CHANNELS, c = chan0 + 2 * lane;
+  const bool on = c < p.C;
+  int n = p.length ? p.length[b] : p.L;
+  n = n < 0 ? 0 : n > p.L ? p.L : n;
+  const int first = blockIdx.y * p.chunk_len, end = min(n, first + p.chunk_len);
+  const Source<T> src[2] = {{reinterpret_cast<const T*>(p.g) + b * p.gb + chan0, p.gt}, {reinterpret_cast<const T*>(p.x) + b * p.xb + chan0, p.xt}};
+  const uint8_t* done = CUT ? p.done + (long long)b * p.L : nullptr;
+#pragma unroll
+  for (int s = 0; s < SLOTS - 1; ++s) {
+    copy_tile<T, 2>(src, p, n, chan0, first + s * PIPE_STEPS, end, slots + s * SLOT_BYTES<T, 2>);
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  }
+  float2 carry = make_float2(0.f, 0.f), product = make_float2(1.f, 1.f);
+  bool any_cut = false;
+  if (!AGG && on && p.h0) carry = pair_of(p.h0 + (long long)b * p.C + c);
+  if (!AGG && p.chunks > 1 && first < n) {
+    const float2* agg = p.agg + (long long)b * p.chunks * p.C + c;
+    const uint8_t* cuts = p.agg_cut + ((long long)b * p.groups + group) * p.chunks;
+#pragma unroll 8
+    for (int i = 0; i < (int)blockIdx.y; ++i) {
+      const float4 m = on ? *reinterpret_cast<const float4*>(agg + (long long)i * p.C) : make_float4(0.f, 0.f, 0.f, 0.f);
+      carry = apply2(make_float2(m.x, m.z), make_float2(m.y, m.w), cuts[i], carry);
+    }
+  }
+  bool flag = CUT && load_flag(p, done, n, first + warp * PIPE_S, lane);
+  T* y = reinterpret_cast<T*>(p.y) + (long long)b * p.L * p.C + c;
+  int slot = 0, par = 0;
+  for (int k0 = first; k0 < end; k0 += PIPE_STEPS, par ^= 1) {
+    asm volatile("cp.async.wait_group %0;" ::"n"(SLOTS - 2) : "memory");
+    __syncthreads();
+    copy_tile<T, 2>(src, p, n, chan0, k0 + (SLOTS - 1) * PIPE_STEPS, end, slots + (slot == 0 ? SLOTS - 1 : slot - 1) * SLOT_BYTES<T, 2>);
+    asm volatile("cp.async.commit_group;" ::: "memory");
+    const int mine = k0 + warp * PIPE_S;
+    unsigned cut = 0;
+    if (CUT) {
+      cut = __ballot_sync(~0u, flag);
+      flag = load_flag(p, done, n, mine + PIPE_STEPS, lane);
+    }
+    const T* sg = reinterpret_cast<const T*>(slots + slot * SLOT_BYTES<T, 2>) + warp * PIPE_S * PIPE_CHANNELS + 2 * lane;
+    const T* sx = sg + PIPE_STEPS * PIPE_CHANNELS;
+    float2 a[PIPE_S], u[PIPE_S];
+#pragma unroll
+    for (int s = 0; s < PIPE_S; ++s) {
+      a[s] = pair_of(sg + s * PIPE_CHANNELS);
+      u[s] = pair_of(sx + s * PIPE_CHANNELS);
+      if (BLEND) {
+        float2 rest;
+        gate_pair2(a[s], a[s], rest);
+        u[s] = mul2(rest, u[s]);
+      }
+    }
+    if (mine + PIPE_S > end) {
+#pragma unroll
+      for (int s = 0; s < PIPE_S; ++s)
+        if (mine + s >= end) {
+          a[s] = make_float2(1.f, 1.f);
+          u[s] = make_float2(0.f, 0.f);
+        }
+    }
+    float2 A = a[0], H = u[0];
+    if (CUT && cut) {
+#pragma unroll
+      for (int s = 1; s < PIPE_S; ++s) {
+        H = apply2(a[s], u[s], cut >> s & 1, H);
+        A = mul2(A, a[s]);
+      }
+    } else {
+#pragma unroll
+      for (int s = 1; s < PIPE_S; ++s) {
+        H = fma2(a[s], H, u[s]);
+        A = mul2(A, a[s]);
+      }
+    }
+    sh.total[par][warp][lane] = make_float4(A.x, A.y, H.x, H.y);
+    if (CUT && lane == 0) sh.cut[par][warp] = cut != 0;
+    __syncthreads();
+    const unsigned long long cuts = CUT ? *reinterpret_cast<const unsigned long long*>(sh.cut[par]) : 0ull;
+    float2 enter = carry;
+    for (int i = 0; i < PIPE_WARPS; ++i) {
+      if (i == warp) enter = carry;
+      const float4 t = sh.total[par][i][lane];
+      const bool cu = CUT && (cuts >> (8 * i) & 1);
+      carry = apply2(make_float2(t.x, t.y), make_float2(t.z, t.w), cu, carry);
+      if (AGG) {
+        product = mul2(product, make_float2(t.x, t.y));
+        any_cut |= cu;
+      }
+    }
+    if constexpr (!AGG) {
+      if (p.states && on && warp == 0) put_pair(p.states + ((long long)b * p.intervals + k0 / MARL_SCAN_INTERVAL) * p.C + c, enter);
+      if (on) {
+        const long long step = p.reverse ? -(long long)p.C : p.C;
+        T* at = y + (long long)(p.reverse ? n - 1 - mine : mine) * p.C;
+        float2 h = enter;
+        if ((CUT && cut) || mine + PIPE_S > end) {
+#pragma unroll
+          for (int s = 0; s < PIPE_S; ++s) {
+            h = apply2(a[s], u[s], CUT && (cut >> s & 1), h);
+            if (mine + s < end) put_pair(at + s * step, h);
+          }
+        } else {
+#pragma unroll
+          for (int s = 0; s < PIPE_S; ++s) {
+            h = fma2(a[s], h, u[s]);
+            put_pair(at + s * step, h);
+          }
+        }
+      }
+    }
+    slot = slot + 1 == SLOTS ? 0 : slot + 1;
+  }
+  asm volatile("cp.async.wait_all;" ::: "memory");
+  if constexpr (AGG) {
+    if (first < end && warp == 0) {
+      if (on) *reinterpret_cast<float4*>(p.agg + ((long long)b * p.chunks + blockIdx.y) * p.C + c) = make_float4(product.x, carry.x, product.y, carry.y);
+      if (lane == 0) p.agg_cut[((long long)b * p.groups + group) * p.chunks + blockIdx.y] = any_cut;
+    }
+    return;
+  }
+  if (!on) return;
+  if (warp == 0 && (n > 0 ? end == n && first < n : blockIdx.y == 0)) {
+    const bool gone = CUT && !p.reverse && n > 0 && done[n - 1];
+    put_pair(p.last + (long long)b * p.C + c, gone ? make_float2(0.f, 0.f) : carry);
+  }
+  const int stop = min(p.L, first + p.chunk_len);
+  for (int t = max(n, first) + warp; t < stop; t += PIPE_WARPS) put_pair(y + (long long)t * p.C, make_float2(0.f, 0.f));
+}
+
+template <typename T, bool BLEND, bool CUT, bool AGG>
+__global__ void __launch_bounds__(PIPE_THREADS, sizeof(T) == 4 ? 2 : 3) scan_pipe_grad_kernel(const __grid_constant__ ScanParams p) {
+  constexpr int SLOTS = PIPE_SLOTS<T>, ARRAYS = AGG ? 2 : 3;
+  extern __shared__ __align__(16) uint8_t slots[];
+  __shared__ PipeShared sh;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int b = blockIdx.x / p.groups, group = blockIdx.x % p.groups, chan0 = group * PIPE_CHANNELS, c = chan0 + 2 * lane;
+  const bool on = c < p.C;
+  int n = p.length ? p.length[b] : p.L;
+  n = n < 0 ? 0 : n > p.L ? p.L : n;
+  const int first = blockIdx.y * p.chunk_len, end = min(n, first + p.chunk_len), used = (n + p.chunk_len - 1) / p.chunk_len;
+  Source<T> src[ARRAYS];
+  src[0] = {reinterpret_cast<const T*>(p.g) + b * p.gb + chan0, p.gt};
+  src[1] = {reinterpret_cast<const T*>(p.dy) + b * p.dyb + chan0, p.dyt};
+  if constexpr (!AGG) src[2] = {reinterpret_cast<const T*>(p.x) + b * p.xb + chan0, p.xt};
+  const uint8_t* done = CUT ? p.done + (long long)b * p.L : nullptr;
+  const int tiles = first < end ? (end - first + PIPE_STEPS - 1) / PIPE_STEPS : 0;
+  auto request = [&](int tile, int into) {  // tiles are taken from the last to the first
+    if (tile >= 0) copy_tile<T, ARRAYS>(src, p, n, chan0, first + tile * PIPE_STEPS, end, slots + into * SLOT_BYTES<T, ARRAYS>);
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+#pragma unroll
+  for (int s = 0; s < SLOTS - 1; ++s) request(tiles - 1 - s, s);
+  const bool gone = CUT && !p.reverse && n > 0 && done[n - 1];
+  float2 carry = make_float2(0.f, 0.f), product = make_float2(1.f, 1.f);
+  bool any_cut = false;
+  if (!AGG && on && p.dlast && !gone) carry = pair_of(p.dlast + (long long)b * p.C + c);
+  if (!AGG && p.chunks > 1 && first < n) {
+    const float2* agg = p.agg + (long long)b * p.chunks * p.C + c;
+    const uint8_t* cuts = p.agg_cut + ((long long)b * p.groups + group) * p.chunks;
+#pragma unroll 8
+    for (int i = used - 1; i > (int)blockIdx.y; --i) {
+      const float4 m = on ? *reinterpret_cast<const float4*>(agg + (long long)i * p.C) : make_float4(0.f, 0.f, 0.f, 0.f);
+      carry = apply2(make_float2(m.x, m.z), make_float2(m.y, m.w), cuts[i], carry);
+    }
+  }
+  auto kept = [&](int k0) {
+    return !AGG && on && k0 >= first ? pair_of(p.states + ((long long)b * p.intervals + k0 / MARL_SCAN_INTERVAL) * p.C + c) : make_float2(0.f, 0.f);
+  };
+  const int last0 = first + (tiles - 1) * PIPE_STEPS;
+  bool flag = CUT && tiles && load_flag(p, done, n, last0 + warp * PIPE_S, lane);
+  float2 state = tiles ? kept(last0) : make_float2(0.f, 0.f);
+  T* dg = reinterpret_cast<T*>(p.dg) + (long long)b * p.L * p.C + c;
+  T* dx = reinterpret_cast<T*>(p.dx) + (long long)b * p.L * p.C + c;
+  int slot = 0, par = 0;
+  for (int i = tiles - 1; i >= 0; --i, par ^= 1) {
+    const int k0 = first + i * PIPE_STEPS, mine = k0 + warp * PIPE_S;
+    asm volatile("cp.async.wait_group %0;" ::"n"(SLOTS - 2) : "memory");
+    __syncthreads();
+    request(i - (SLOTS - 1), slot == 0 ? SLOTS - 1 : slot - 1);
+    unsigned cut = 0;
+    if (CUT) {
+      cut = __ballot_sync(~0u, flag);
+      flag = i > 0 && load_flag(p, done, n, mine - PIPE_STEPS, lane);
+    }
+    float2 enter = state;
+    if (i > 0) state = kept(k0 - PIPE_STEPS);
+    const T* sg = reinterpret_cast<const T*>(slots + slot * SLOT_BYTES<T, ARRAYS>) + warp * PIPE_S * PIPE_CHANNELS + 2 * lane;
+    const T *sd = sg + PIPE_STEPS * PIPE_CHANNELS, *sx = sd + PIPE_STEPS * PIPE_CHANNELS;
+    const bool full = mine + PIPE_S <= end;
+    // (dy and x of steps behind the end: the slot holds something older)
+    auto d_of = [&](int s) { return full || mine + s < end ? pair_of(sd + s * PIPE_CHANNELS) : make_float2(0.f, 0.f); };
+    auto x_of = [&](int s) { return full || mine + s < end ? pair_of(sx + s * PIPE_CHANNELS) : make_float2(0.f, 0.f); };
+    float2 a[PIPE_S], q[BLEND ? PIPE_S : 1];
+#pragma unroll
+    for (int s = 0; s < PIPE_S; ++s) {
+      a[s] = full || mine + s < end ? pair_of(sg + s * PIPE_CHANNELS) : make_float2(0.f, 0.f);
+      if (BLEND) gate_pair2(a[s], a[s], q[s]);
+      if (!full && mine + s >= end) a[s] = make_float2(1.f, 1.f);
+    }
+    float2 A = a[0], H = make_float2(0.f, 0.f), R = make_float2(0.f, 0.f);
+#pragma unroll
+    for (int s = 1; s < PIPE_S; ++s) A = mul2(A, a[s]);
+    if constexpr (!AGG) {
+#pragma unroll
+      for (int s = 0; s < PIPE_S; ++s) {
+        const float2 u = BLEND ? mul2(q[s], x_of(s)) : x_of(s);
+        H = apply2(a[s], u, CUT && (cut >> s & 1), H);
+      }
+    }
+#pragma unroll
+    for (int s = PIPE_S - 1; s >= 0; --s) {
+      R = mul2(a[s], add2(d_of(s), R));
+      if (CUT && (cut >> s & 1)) R = make_float2(0.f, 0.f);
+    }
+    sh.total[par][warp][lane] = make_float4(A.x, A.y, H.x, H.y);
+    sh.back[par][warp][lane] = R;
+    if (CUT && lane == 0) sh.cut[par][warp] = cut != 0;
+    __syncthreads();
+    const unsigned long long cuts = CUT ? *reinterpret_cast<const unsigned long long*>(sh.cut[par]) : 0ull;
+    if (!AGG)
+      for (int j = 0; j < warp; ++j) {
+        const float4 t = sh.total[par][j][lane];
+        enter = apply2(make_float2(t.x, t.y), make_float2(t.z, t.w), CUT && (cuts >> (8 * j) & 1), enter);
+      }
+    float2 back = carry;
+    for (int j = PIPE_WARPS - 1; j >= 0; --j) {
+      if (j == warp) back = carry;
+      const float2 f = *reinterpret_cast<const float2*>(&sh.total[par][j][lane]);
+      const bool cu = CUT && (cuts >> (8 * j) & 1);
+      carry = apply2(f, sh.back[par][j][lane], cu, carry);
+      if (AGG) {
+        product = mul2(product, f);
+        any_cut |= cu;
+      }
+    }
+    if constexpr (!AGG) {
+      if (on) {
+        const long long step = p.reverse ? -(long long)p.C : p.C;
+        const long long at = (long long)(p.reverse ? n - 1 - mine : mine) * p.C;
+        float2 G[PIPE_S];
+#pragma unroll
+        for (int s = PIPE_S - 1; s >= 0; --s) {
+          G[s] = add2(d_of(s), back);
+          back = mul2(a[s], G[s]);
+          if (CUT && (cut >> s & 1)) back = make_float2(0.f, 0.f);
+        }
+        float2 h = enter;
+#pragma unroll
+        for (int s = 0; s < PIPE_S; ++s) {
+          if (CUT && (cut >> s & 1)) h = make_float2(0.f, 0.f);
+          const float2 x = x_of(s);
+          float2 og, ox;
+          if (BLEND) {
+            ox = mul2(G[s], q[s]);
+            og = mul2(add2(h, make_float2(-x.x, -x.y)), mul2(a[s], ox));
+            h = fma2(a[s], h, mul2(q[s], x));
+          } else {
+            ox = G[s];
+            og = mul2(G[s], h);
+            h = fma2(a[s], h, x);
+          }
+          if (full || mine + s < end) {
+            put_pair(dg + at + s * step, og);
+            put_pair(dx + at + s * step, ox);
+          }
+        }
+      }
+    }
+    slot = slot + 1 == SLOTS ? 0 : slot + 1;
+  }
+  asm volatile("cp.async.wait_all;" ::: "memory");
+  if constexpr (AGG) {
+    if (first < end && warp == 0) {
+      if (on) *reinterpret_cast<float4*>(p.agg + ((long long)b * p.chunks + blockIdx.y) * p.C + c) = make_float4(product.x, carry.x, product.y, carry.y);
+      if (lane == 0) p.agg_cut[((long long)b * p.groups + group) * p.chunks + blockIdx.y] = any_cut;
+    }
+    return;
+  }
+  if (!on) return;
+  if (warp == 0 && blockIdx.y == 0 && p.dh0) put_pair(p.dh0 + (long long)b * p.C + c, carry);
+  const int stop = min(p.L, first + p.chunk_len);
+  for (int t = max(n, first) + warp; t < stop; t += PIPE_WARPS) {
+    put_pair(dg + (long long)t * p.C, make_float2(0.f, 0.f));
+    put_pair(dx + (long long)t * p.C, make_float2(0.f, 0.f));
+  }
+}
+
 // How a call is laid out.  V: channels a lane.
-static void plan(ScanParams& p, int V) {
+static void plan(ScanParams& p, int V, bool pipe) {
   const int lanes = (p.C + V - 1) / V;
+  p.pipe = pipe;
+  // Lanes along the channels: 32, or fewer where that leaves at least a quarter fewer lanes idle.
   p.lg = 0;
   while ((1 << p.lg) < lanes && p.lg < 5) ++p.lg;
+  for (int lg = p.lg - 1; lg >= 3; --lg) {
+    const long long now = (long long)((lanes + (1 << p.lg) - 1) >> p.lg) << p.lg, then = (long long)((lanes + (1 << lg) - 1) >> lg) << lg;
+    if (4 * then <= 3 * now) p.lg = lg;
+  }
   p.groups = (lanes + (1 << p.lg) - 1) >> p.lg;
-  const int warp_steps = (32 >> p.lg) * STEPS;
+  p.steps = p.L <= 1 ? 1 : STEPS;
+  const int warp_steps = (32 >> p.lg) * p.steps;
   p.warps = 1;
   while (p.warps < MAX_WARPS && p.warps * warp_steps < p.L) p.warps *= 2;
   p.units = MAX_WARPS / p.warps;
+  if (pipe) {
+    p.lg = 5;
+    p.groups = (p.C + PIPE_CHANNELS - 1) / PIPE_CHANNELS;
+    p.steps = PIPE_S;
+    p.warps = PIPE_WARPS;
+    p.units = 1;
+  }
   p.intervals = (p.L + MARL_SCAN_INTERVAL - 1) / MARL_SCAN_INTERVAL;
   // Few sequences and channels: the time axis is divided over blocks, which takes a launch for the chunks' maps and reads
   // gate and x twice.
-  const int tile = p.warps * warp_steps;   // a multiple of MARL_SCAN_INTERVAL wherever there are two
+  const int tile = pipe ? PIPE_STEPS : p.warps * warp_steps;   // a multiple of MARL_SCAN_INTERVAL wherever there are two
   const long long blocks = ((long long)p.B * p.groups + p.units - 1) / p.units;
   p.chunks = 1;
   p.chunk_len = p.L > 0 ? p.L : 1;
@@ -571,14 +942,22 @@ static int channels_a_lane(const marl_scan_t* in) {
   return pairs ? 2 : 1;
 }
 
-static ScanParams scan_params(const marl_scan_t* in, int V) {
+// Tiles by asynchronous copies: 16-byte pieces of rows everywhere, and enough channels and steps to fill tiles of 64 x 64.
+static bool can_pipe(const marl_scan_t* in) {
+  const long long es = (long long)dtype_bytes(in->dtype);
+  auto whole = [&](long long elements) { return elements * es % 16 == 0; };
+  return in->C >= 48 && in->L >= 32 && in->gate_c == 1 && in->x_c == 1 && whole(in->C) && whole(in->gate_b) && whole(in->gate_t) && whole(in->x_b) &&
+         whole(in->x_t) && !misaligned(in->gate, 16) && !misaligned(in->x, 16) && !misaligned(in->h0, 8);
+}
+
+static ScanParams scan_params(const marl_scan_t* in, int V, bool pipe) {
   ScanParams p = {};
   p.g = in->gate; p.x = in->x;
   p.gb = in->gate_b; p.gt = in->gate_t; p.xb = in->x_b; p.xt = in->x_t;
   p.gc = in->gate_c; p.xc = in->x_c;
   p.h0 = in->h0; p.done = in->done; p.length = in->length;
   p.B = in->B; p.L = in->L; p.C = in->C; p.reverse = in->reverse != 0;
-  plan(p, V);
+  plan(p, V, pipe);
   return p;
 }
 
@@ -594,7 +973,7 @@ static int set_work(ScanParams& p, void* work, size_t bytes) {
   const size_t need = work_need(p);
   if (!need) return MARL_OK;
   if (!work || bytes < need) return fail(MARL_ENOMEM, "work: %zu bytes given, %zu needed", work ? bytes : (size_t)0, need);
-  if (misaligned(work, 8)) return fail(MARL_EALIGN, "work must be 8-byte aligned");
+  if (misaligned(work, 16)) return fail(MARL_EALIGN, "work must be 16-byte aligned");
   p.agg = reinterpret_cast<float2*>(work);
   p.agg_cut = reinterpret_cast<uint8_t*>(p.agg + (size_t)p.B * p.chunks * p.C);
   return MARL_OK;
@@ -605,20 +984,59 @@ static int launch_ok(const char* what) {
   return e == cudaSuccess ? MARL_OK : fail(MARL_ECUDA, "%s: %s", what, cudaGetErrorString(e));
 }
 
-template <typename T, int V, bool BLEND>
-static int run_scan(const ScanParams& p, bool grad, cudaStream_t stream) {
+template <typename T, int V, int S, bool BLEND, bool CUT>
+static int launch_scan(const ScanParams& p, bool grad, cudaStream_t stream) {
   const long long blocks = ((long long)p.B * p.groups + p.units - 1) / p.units;
   if (blocks > INT32_MAX || p.chunks > 65535) return fail(MARL_EINVAL, "too many sequences or channels");
   const dim3 grid((unsigned)blocks, (unsigned)p.chunks);
   const int threads = p.units * p.warps * 32;
   if (!grad) {
-    if (p.chunks > 1) scan_kernel<T, V, BLEND, true><<<grid, threads, 0, stream>>>(p);
-    scan_kernel<T, V, BLEND, false><<<grid, threads, 0, stream>>>(p);
+    if constexpr (S > 1)
+      if (p.chunks > 1) scan_kernel<T, V, S, BLEND, CUT, true><<<grid, threads, 0, stream>>>(p);
+    scan_kernel<T, V, S, BLEND, CUT, false><<<grid, threads, 0, stream>>>(p);
     return launch_ok("marl_linear_scan");
   }
-  if (p.chunks > 1) scan_grad_kernel<T, V, BLEND, true><<<grid, threads, 0, stream>>>(p);
-  scan_grad_kernel<T, V, BLEND, false><<<grid, threads, 0, stream>>>(p);
+  if constexpr (S > 1)
+    if (p.chunks > 1) scan_grad_kernel<T, V, S, BLEND, CUT, true><<<grid, threads, 0, stream>>>(p);
+  scan_grad_kernel<T, V, S, BLEND, CUT, false><<<grid, threads, 0, stream>>>(p);
   return launch_ok("marl_linear_scan_backward");
+}
+
+static uint32_t g_pipe_smem[3][16][SMEM_OPTIN_DEVICES];
+
+template <typename T, bool BLEND, bool CUT>
+static int launch_pipe(const ScanParams& p, bool grad, int which, cudaStream_t stream) {
+  const long long blocks = (long long)p.B * p.groups;
+  if (blocks > INT32_MAX || p.chunks > 65535) return fail(MARL_EINVAL, "too many sequences or channels");
+  const dim3 grid((unsigned)blocks, (unsigned)p.chunks);
+  const int w = (BLEND ? 2 : 0) + (CUT ? 1 : 0);
+  auto go = [&](auto kernel, int bytes, int index) {
+    // (one table entry per kernel: the maps' launch of the gradient needs less than the gradient)
+    const cudaError_t e = ensure_dynamic_smem(reinterpret_cast<const void*>(kernel), (uint32_t)bytes, g_pipe_smem[which][index]);
+    if (e != cudaSuccess) return e;
+    kernel<<<grid, PIPE_THREADS, bytes, stream>>>(p);
+    return cudaGetLastError();
+  };
+  cudaError_t e = cudaSuccess;
+  constexpr int two = PIPE_SLOTS<T> * SLOT_BYTES<T, 2>, three = PIPE_SLOTS<T> * SLOT_BYTES<T, 3>;
+  if (!grad) {
+    if (p.chunks > 1) e = go(scan_pipe_kernel<T, BLEND, CUT, true>, two, w);
+    if (e == cudaSuccess) e = go(scan_pipe_kernel<T, BLEND, CUT, false>, two, w + 4);
+  } else {
+    if (p.chunks > 1) e = go(scan_pipe_grad_kernel<T, BLEND, CUT, true>, two, w + 8);
+    if (e == cudaSuccess) e = go(scan_pipe_grad_kernel<T, BLEND, CUT, false>, three, w + 12);
+  }
+  return e == cudaSuccess ? MARL_OK : fail(MARL_ECUDA, "marl_linear_scan%s: %s", grad ? "_backward" : "", cudaGetErrorString(e));
+}
+
+template <typename T, int V, bool BLEND>
+static int run_scan(const ScanParams& p, bool grad, cudaStream_t stream) {
+  if (p.pipe) {
+    constexpr int which = sizeof(T) == 4 ? 0 : std::is_same<T, __half>::value ? 1 : 2;
+    return p.done ? launch_pipe<T, BLEND, true>(p, grad, which, stream) : launch_pipe<T, BLEND, false>(p, grad, which, stream);
+  }
+  if (p.steps == 1) return p.done ? launch_scan<T, V, 1, BLEND, true>(p, grad, stream) : launch_scan<T, V, 1, BLEND, false>(p, grad, stream);
+  return p.done ? launch_scan<T, V, STEPS, BLEND, true>(p, grad, stream) : launch_scan<T, V, STEPS, BLEND, false>(p, grad, stream);
 }
 
 static int dispatch(const ScanParams& p, int dtype, int V, bool blend, bool grad, cudaStream_t stream) {
@@ -640,8 +1058,8 @@ extern "C" int marl_linear_scan_query(const marl_scan_t* in, size_t* states_byte
   if (rc != MARL_OK) return rc;
   if (states_bytes) *states_bytes = (size_t)in->B * (((size_t)in->L + MARL_SCAN_INTERVAL - 1) / MARL_SCAN_INTERVAL) * in->C * 4;
   if (work_bytes) {  // whatever the arrays' alignment turns out to be
-    const size_t one = work_need(scan_params(in, 1)), two = in->dtype == MARL_DTYPE_FP32 ? 0 : work_need(scan_params(in, 2));
-    *work_bytes = std::max(one, two);
+    const size_t one = work_need(scan_params(in, 1, false)), two = in->dtype == MARL_DTYPE_FP32 ? 0 : work_need(scan_params(in, 2, false));
+    *work_bytes = std::max(work_need(scan_params(in, 2, true)), std::max(one, two));
   }
   return MARL_OK;
 }
@@ -655,7 +1073,7 @@ extern "C" int marl_linear_scan(void* stream, const marl_scan_t* in, void* y, fl
   if (misaligned(y, dtype_bytes(in->dtype)) || misaligned(last, 4) || misaligned(states, 4))
     return fail(MARL_EALIGN, "an output is not aligned to its elements");
   const int V = channels_a_lane(in) == 2 && !misaligned(y, 4) ? 2 : 1;
-  ScanParams p = scan_params(in, V);
+  ScanParams p = scan_params(in, V, can_pipe(in) && !misaligned(y, 8) && !misaligned(last, 8) && !misaligned(states, 8));
   p.y = y;
   p.last = last;
   p.states = states;
@@ -676,7 +1094,9 @@ extern "C" int marl_linear_scan_backward(void* stream, const marl_scan_t* in, co
     return fail(MARL_EALIGN, "an array is not aligned to its elements");
   const bool pairs = channels_a_lane(in) == 2 && dy_b % 2 == 0 && dy_t % 2 == 0 && !misaligned(dy, 4) && !misaligned(dgate, 4) && !misaligned(dx, 4);
   const int V = pairs ? 2 : 1;
-  ScanParams p = scan_params(in, V);
+  const bool pipe = can_pipe(in) && dy_b * (long long)es % 16 == 0 && dy_t * (long long)es % 16 == 0 && !misaligned(dy, 16) && !misaligned(dgate, 8) &&
+                    !misaligned(dx, 8) && !misaligned(states, 8) && !misaligned(dlast, 8) && !misaligned(dh0, 8);
+  ScanParams p = scan_params(in, V, pipe);
   p.states = const_cast<float*>(states);
   p.dy = dy;
   p.dyb = dy_b;

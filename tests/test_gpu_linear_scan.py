@@ -129,7 +129,8 @@ def test_scan_and_gradient(B, L, C, dt):
 
 
 @pytest.mark.parametrize("B,L,C,dt,form", [(1, 4100, 32, "fp32", "raw"), (2, 5003, 6, "bf16", "blend"), (1, 9001, 1, "fp32", "blend"),
-                                           (3, 2500, 70, "fp16", "raw"), (1, 3333, 64, "bf16", "raw")])
+                                           (3, 2500, 70, "fp16", "raw"), (1, 3333, 64, "bf16", "raw"),
+                                           (1, 5001, 200, "fp32", "blend"), (2, 3100, 72, "fp16", "blend")])
 def test_time_divided_over_blocks(B, L, C, dt, form):
     for reverse in (False, True):
         gate, x, kw, dy, dlast = _make(B, L, C, dt, form, L, done=reverse, ragged=B > 1)
@@ -139,6 +140,17 @@ def test_time_divided_over_blocks(B, L, C, dt, form):
     gate, x, kw, dy, dlast = _make(B, L, C, dt, form, L + 1, done=True, ragged=False)
     kw["done"][:, 100:L - 100] = 0     # cuts at the ends only: maps without one over many blocks
     _check(gate, x, kw, dy, dlast, form, False)
+
+
+@pytest.mark.parametrize("dt", ["fp32", "bf16", "fp16"])
+@pytest.mark.parametrize("B,L,C", [(3, 32, 48), (4, 64, 64), (3, 65, 72), (5, 127, 128), (4, 300, 200), (2, 1000, 64), (300, 40, 64)])
+def test_rows_on_16_byte_boundaries(B, L, C, dt):
+    """Tiles by asynchronous copies: whole and partial tiles and groups of channels, either direction, cuts and ends."""
+    for form in ("raw", "blend"):
+        for reverse in (False, True):
+            for done, ragged, fused in ((True, True, False), (False, True, True), (True, False, True)):
+                gate, x, kw, dy, dlast = _make(B, L, C, dt, form, B + L + C, done, ragged, fused)
+                _check(gate, x, kw, dy, dlast, form, reverse)
 
 
 @pytest.mark.parametrize("form", ["raw", "blend"])
