@@ -37,7 +37,6 @@ struct ScanParams {
   int lg;          // log2 of the lanes along the channels
   int warps;       // warps along time
   int pipe;        // tiles by asynchronous copies
-  int steps;       // steps a thread holds: 1 (calls of one step) or STEPS
   int units;       // units (sequence, group of channels) a block
   int groups;      // groups of channels a sequence
   int chunks, chunk_len, intervals;
@@ -517,11 +516,73 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 2) scan_grad_kernel(const __gr
   }
 }
 
+// ---- calls of one step: the serving form, element by element --------------------------------------------------------
+template <typename T, int V, bool BLEND>
+__global__ void scan_step_kernel(const __grid_constant__ ScanParams p) {
+  const int c = (blockIdx.x * blockDim.x + threadIdx.x) * V;
+  if (c >= p.C) return;
+  for (int b = blockIdx.y * blockDim.y + threadIdx.y; b < p.B; b += gridDim.y * blockDim.y) {
+    const bool live = !p.length || p.length[b] > 0, done = live && p.done && p.done[b];
+    const long long at = (long long)b * p.C + c;
+    float g[V] = {}, x[V] = {}, y[V];
+    if (live) {
+      unpack(*reinterpret_cast<const Raw<T, V>*>(reinterpret_cast<const T*>(p.g) + b * p.gb + (long long)c * p.gc), g);
+      unpack(*reinterpret_cast<const Raw<T, V>*>(reinterpret_cast<const T*>(p.x) + b * p.xb + (long long)c * p.xc), x);
+    }
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      const float h0 = p.h0 ? p.h0[at + v] : 0.f;
+      float a, u;
+      step_ab<BLEND>(true, g[v], x[v], a, u);
+      const float h = p.reverse && done ? u : fmaf(a, h0, u);
+      if (live && p.states) p.states[at + v] = h0;
+      p.last[at + v] = !live ? h0 : !p.reverse && done ? 0.f : h;
+      y[v] = live ? h : 0.f;
+    }
+    put(reinterpret_cast<T*>(p.y) + at, y);
+  }
+}
+
+template <typename T, int V, bool BLEND>
+__global__ void scan_step_grad_kernel(const __grid_constant__ ScanParams p) {
+  const int c = (blockIdx.x * blockDim.x + threadIdx.x) * V;
+  if (c >= p.C) return;
+  for (int b = blockIdx.y * blockDim.y + threadIdx.y; b < p.B; b += gridDim.y * blockDim.y) {
+    const bool live = !p.length || p.length[b] > 0, done = live && p.done && p.done[b];
+    const long long at = (long long)b * p.C + c;
+    float g[V] = {}, x[V] = {}, d[V] = {}, dg[V], dx[V];
+    if (live) {
+      unpack(*reinterpret_cast<const Raw<T, V>*>(reinterpret_cast<const T*>(p.g) + b * p.gb + (long long)c * p.gc), g);
+      unpack(*reinterpret_cast<const Raw<T, V>*>(reinterpret_cast<const T*>(p.x) + b * p.xb + (long long)c * p.xc), x);
+      unpack(*reinterpret_cast<const Raw<T, V>*>(reinterpret_cast<const T*>(p.dy) + b * p.dyb + c), d);
+    }
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      const float dl = p.dlast ? p.dlast[at + v] : 0.f;
+      const float G = d[v] + (!p.reverse && done ? 0.f : dl), came = live && !(p.reverse && done) ? p.states[at + v] : 0.f;
+      float a = g[v], rest = 1.f;
+      if (BLEND) gate_pair(g[v], a, rest);
+      dg[v] = !live ? 0.f : BLEND ? (came - x[v]) * (a * (G * rest)) : G * came;
+      dx[v] = !live ? 0.f : G * rest;
+      if (p.dh0) p.dh0[at + v] = !live ? dl : p.reverse && done ? 0.f : a * G;
+    }
+    put(reinterpret_cast<T*>(p.dg) + at, dg);
+    put(reinterpret_cast<T*>(p.dx) + at, dx);
+  }
+}
+
 // ---- aligned rows of many channels: tiles by asynchronous copies ----------------------------------------------------
 // A block takes 64 channels of a sequence, two a lane, in tiles of 64 steps, eight steps a warp.  The tiles of gate, x (and dy) come in
 // 16 bytes a copy into a ring of slots in shared memory, ahead of the tile that is computed; the arithmetic is packed, two channels
 // an operation.  The gradient reads x and dy from the slot twice rather than holding them.
 constexpr int PIPE_STEPS = 64, PIPE_CHANNELS = 64, PIPE_THREADS = 256, PIPE_WARPS = 8, PIPE_S = PIPE_STEPS / PIPE_WARPS;
+#ifndef PB
+#define PB 4
+#endif
+constexpr int PIPE_BLOCKS = PB;
+#ifndef PG
+#define PG 3
+#endif
 template <typename T> constexpr int PIPE_SLOTS = sizeof(T) == 4 ? 2 : 3;
 template <typename T, int ARRAYS> constexpr int SLOT_BYTES = ARRAYS * PIPE_STEPS * PIPE_CHANNELS * (int)sizeof(T);
 
@@ -583,8 +644,38 @@ __device__ __forceinline__ bool load_flag(const ScanParams& p, const uint8_t* do
 
 __device__ __forceinline__ float2 apply2(float2 a, float2 h, bool cut, float2 in) { return cut ? h : fma2(a, in, h); }
 
+// The state that enters a chunk (BACK: the gradient that comes back into it) behind `count` others: the warps compose an eighth of them each.
+template <bool BACK>
+__device__ __forceinline__ float2 enter_chunk2(const ScanParams& p, PipeShared& sh, int b, int group, int c, bool on, int count, float2 carry,
+                                               int used = 0) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const float2* agg = p.agg + (long long)b * p.chunks * p.C + c;
+  const uint8_t* cuts = p.agg_cut + ((long long)b * p.groups + group) * p.chunks;
+  const int per = (count + PIPE_WARPS - 1) / PIPE_WARPS, i0 = warp * per, i1 = min(count, i0 + per);
+  float2 A = make_float2(1.f, 1.f), H = make_float2(0.f, 0.f);
+  bool cut = false;
+#pragma unroll 8
+  for (int i = i0; i < i1; ++i) {
+    const int at = BACK ? used - 1 - i : i;
+    const float4 m = on ? *reinterpret_cast<const float4*>(agg + (long long)at * p.C) : make_float4(0.f, 0.f, 0.f, 0.f);
+    const bool cu = cuts[at];
+    H = apply2(make_float2(m.x, m.z), make_float2(m.y, m.w), cu, H);
+    A = mul2(A, make_float2(m.x, m.z));
+    cut |= cu;
+  }
+  sh.total[0][warp][lane] = make_float4(A.x, A.y, H.x, H.y);
+  if (lane == 0) sh.cut[0][warp] = cut;
+  __syncthreads();
+  for (int i = 0; i < PIPE_WARPS; ++i) {
+    const float4 t = sh.total[0][i][lane];
+    carry = apply2(make_float2(t.x, t.y), make_float2(t.z, t.w), sh.cut[0][i], carry);
+  }
+  __syncthreads();
+  return carry;
+}
+
 template <typename T, bool BLEND, bool CUT, bool AGG>
-__global__ void __launch_bounds__(PIPE_THREADS, 3) scan_pipe_kernel(const __grid_constant__ ScanParams p) {
+__global__ void __launch_bounds__(PIPE_THREADS, PIPE_BLOCKS) scan_pipe_kernel(const __grid_constant__ ScanParams p) {
   constexpr int SLOTS = PIPE_SLOTS<T>;
   extern __shared__ __align__(16) uint8_t slots[];
   __shared__ PipeShared sh;
@@ -604,15 +695,7 @@ __global__ void __launch_bounds__(PIPE_THREADS, 3) scan_pipe_kernel(const __grid
   float2 carry = make_float2(0.f, 0.f), product = make_float2(1.f, 1.f);
   bool any_cut = false;
   if (!AGG && on && p.h0) carry = pair_of(p.h0 + (long long)b * p.C + c);
-  if (!AGG && p.chunks > 1 && first < n) {
-    const float2* agg = p.agg + (long long)b * p.chunks * p.C + c;
-    const uint8_t* cuts = p.agg_cut + ((long long)b * p.groups + group) * p.chunks;
-#pragma unroll 8
-    for (int i = 0; i < (int)blockIdx.y; ++i) {
-      const float4 m = on ? *reinterpret_cast<const float4*>(agg + (long long)i * p.C) : make_float4(0.f, 0.f, 0.f, 0.f);
-      carry = apply2(make_float2(m.x, m.z), make_float2(m.y, m.w), cuts[i], carry);
-    }
-  }
+  if (!AGG && p.chunks > 1 && first < n) carry = enter_chunk2<false>(p, sh, b, group, c, on, blockIdx.y, carry);
   bool flag = CUT && load_flag(p, done, n, first + warp * PIPE_S, lane);
   T* y = reinterpret_cast<T*>(p.y) + (long long)b * p.L * p.C + c;
   int slot = 0, par = 0;
@@ -718,7 +801,7 @@ __global__ void __launch_bounds__(PIPE_THREADS, 3) scan_pipe_kernel(const __grid
 }
 
 template <typename T, bool BLEND, bool CUT, bool AGG>
-__global__ void __launch_bounds__(PIPE_THREADS, sizeof(T) == 4 ? 2 : 3) scan_pipe_grad_kernel(const __grid_constant__ ScanParams p) {
+__global__ void __launch_bounds__(PIPE_THREADS, sizeof(T) == 4 ? 2 : PG) scan_pipe_grad_kernel(const __grid_constant__ ScanParams p) {
   constexpr int SLOTS = PIPE_SLOTS<T>, ARRAYS = AGG ? 2 : 3;
   extern __shared__ __align__(16) uint8_t slots[];
   __shared__ PipeShared sh;
@@ -744,15 +827,7 @@ __global__ void __launch_bounds__(PIPE_THREADS, sizeof(T) == 4 ? 2 : 3) scan_pip
   float2 carry = make_float2(0.f, 0.f), product = make_float2(1.f, 1.f);
   bool any_cut = false;
   if (!AGG && on && p.dlast && !gone) carry = pair_of(p.dlast + (long long)b * p.C + c);
-  if (!AGG && p.chunks > 1 && first < n) {
-    const float2* agg = p.agg + (long long)b * p.chunks * p.C + c;
-    const uint8_t* cuts = p.agg_cut + ((long long)b * p.groups + group) * p.chunks;
-#pragma unroll 8
-    for (int i = used - 1; i > (int)blockIdx.y; --i) {
-      const float4 m = on ? *reinterpret_cast<const float4*>(agg + (long long)i * p.C) : make_float4(0.f, 0.f, 0.f, 0.f);
-      carry = apply2(make_float2(m.x, m.z), make_float2(m.y, m.w), cuts[i], carry);
-    }
-  }
+  if (!AGG && p.chunks > 1 && first < n) carry = enter_chunk2<true>(p, sh, b, group, c, on, used - 1 - (int)blockIdx.y, carry, used);
   auto kept = [&](int k0) {
     return !AGG && on && k0 >= first ? pair_of(p.states + ((long long)b * p.intervals + k0 / MARL_SCAN_INTERVAL) * p.C + c) : make_float2(0.f, 0.f);
   };
@@ -887,15 +962,13 @@ static void plan(ScanParams& p, int V, bool pipe) {
     if (4 * then <= 3 * now) p.lg = lg;
   }
   p.groups = (lanes + (1 << p.lg) - 1) >> p.lg;
-  p.steps = p.L <= 1 ? 1 : STEPS;
-  const int warp_steps = (32 >> p.lg) * p.steps;
+  const int warp_steps = (32 >> p.lg) * STEPS;
   p.warps = 1;
   while (p.warps < MAX_WARPS && p.warps * warp_steps < p.L) p.warps *= 2;
   p.units = MAX_WARPS / p.warps;
   if (pipe) {
     p.lg = 5;
     p.groups = (p.C + PIPE_CHANNELS - 1) / PIPE_CHANNELS;
-    p.steps = PIPE_S;
     p.warps = PIPE_WARPS;
     p.units = 1;
   }
@@ -908,8 +981,8 @@ static void plan(ScanParams& p, int V, bool pipe) {
   p.chunk_len = p.L > 0 ? p.L : 1;
   if (blocks < 2 * SCAN_SMS && p.L >= 4 * tile) {
     const int tiles = (p.L + tile - 1) / tile;
-    int want = (int)((4 * SCAN_SMS + blocks - 1) / blocks);
-    want = std::min(want, tiles / 2);
+    int want = (int)((pipe ? 3 : 4) * SCAN_SMS / blocks);
+    want = std::max(1, std::min(want, tiles / 2));
     const int per = (tiles + want - 1) / want;
     p.chunk_len = per * tile;
     p.chunks = (p.L + p.chunk_len - 1) / p.chunk_len;
@@ -991,13 +1064,11 @@ static int launch_scan(const ScanParams& p, bool grad, cudaStream_t stream) {
   const dim3 grid((unsigned)blocks, (unsigned)p.chunks);
   const int threads = p.units * p.warps * 32;
   if (!grad) {
-    if constexpr (S > 1)
-      if (p.chunks > 1) scan_kernel<T, V, S, BLEND, CUT, true><<<grid, threads, 0, stream>>>(p);
+    if (p.chunks > 1) scan_kernel<T, V, S, BLEND, CUT, true><<<grid, threads, 0, stream>>>(p);
     scan_kernel<T, V, S, BLEND, CUT, false><<<grid, threads, 0, stream>>>(p);
     return launch_ok("marl_linear_scan");
   }
-  if constexpr (S > 1)
-    if (p.chunks > 1) scan_grad_kernel<T, V, S, BLEND, CUT, true><<<grid, threads, 0, stream>>>(p);
+  if (p.chunks > 1) scan_grad_kernel<T, V, S, BLEND, CUT, true><<<grid, threads, 0, stream>>>(p);
   scan_grad_kernel<T, V, S, BLEND, CUT, false><<<grid, threads, 0, stream>>>(p);
   return launch_ok("marl_linear_scan_backward");
 }
@@ -1018,7 +1089,8 @@ static int launch_pipe(const ScanParams& p, bool grad, int which, cudaStream_t s
     return cudaGetLastError();
   };
   cudaError_t e = cudaSuccess;
-  constexpr int two = PIPE_SLOTS<T> * SLOT_BYTES<T, 2>, three = PIPE_SLOTS<T> * SLOT_BYTES<T, 3>;
+  const int slots = std::min(PIPE_SLOTS<T>, (std::min(p.L, p.chunk_len) + PIPE_STEPS - 1) / PIPE_STEPS);  // no more than there are tiles
+  const int two = slots * SLOT_BYTES<T, 2>, three = slots * SLOT_BYTES<T, 3>;
   if (!grad) {
     if (p.chunks > 1) e = go(scan_pipe_kernel<T, BLEND, CUT, true>, two, w);
     if (e == cudaSuccess) e = go(scan_pipe_kernel<T, BLEND, CUT, false>, two, w + 4);
@@ -1035,7 +1107,17 @@ static int run_scan(const ScanParams& p, bool grad, cudaStream_t stream) {
     constexpr int which = sizeof(T) == 4 ? 0 : std::is_same<T, __half>::value ? 1 : 2;
     return p.done ? launch_pipe<T, BLEND, true>(p, grad, which, stream) : launch_pipe<T, BLEND, false>(p, grad, which, stream);
   }
-  if (p.steps == 1) return p.done ? launch_scan<T, V, 1, BLEND, true>(p, grad, stream) : launch_scan<T, V, 1, BLEND, false>(p, grad, stream);
+  if (p.L == 1) {
+    const int pairs = (p.C + V - 1) / V;
+    int tx = 32;
+    while (tx < 256 && tx < pairs) tx *= 2;
+    const dim3 threads((unsigned)tx, (unsigned)(256 / tx));
+    const unsigned gy = (unsigned)std::min<long long>(((long long)p.B + threads.y - 1) / threads.y, 65535);
+    const dim3 grid((unsigned)((pairs + tx - 1) / tx), gy);
+    if (grad) scan_step_grad_kernel<T, V, BLEND><<<grid, threads, 0, stream>>>(p);
+    else scan_step_kernel<T, V, BLEND><<<grid, threads, 0, stream>>>(p);
+    return launch_ok("marl_linear_scan of one step");
+  }
   return p.done ? launch_scan<T, V, STEPS, BLEND, true>(p, grad, stream) : launch_scan<T, V, STEPS, BLEND, false>(p, grad, stream);
 }
 
