@@ -576,13 +576,7 @@ __global__ void scan_step_grad_kernel(const __grid_constant__ ScanParams p) {
 // 16 bytes a copy into a ring of slots in shared memory, ahead of the tile that is computed; the arithmetic is packed, two channels
 // an operation.  The gradient reads x and dy from the slot twice rather than holding them.
 constexpr int PIPE_STEPS = 64, PIPE_CHANNELS = 64, PIPE_THREADS = 256, PIPE_WARPS = 8, PIPE_S = PIPE_STEPS / PIPE_WARPS;
-#ifndef PB
-#define PB 4
-#endif
-constexpr int PIPE_BLOCKS = PB;
-#ifndef PG
-#define PG 3
-#endif
+constexpr int PIPE_BLOCKS = 4;
 template <typename T> constexpr int PIPE_SLOTS = sizeof(T) == 4 ? 2 : 3;
 template <typename T, int ARRAYS> constexpr int SLOT_BYTES = ARRAYS * PIPE_STEPS * PIPE_CHANNELS * (int)sizeof(T);
 
@@ -612,29 +606,28 @@ struct PipeShared {
   __align__(8) uint8_t cut[2][PIPE_WARPS];
 };
 
-// What a block copies: row `k` (scan order) of an array at base + t stride, its 64 channels from chan0 on.
+// One array's tiles, as a thread copies them: 16 bytes of a row of the tile, and of the rows ROW_STEP further on.
 template <typename T>
 struct Source {
-  const T* base;
-  long long stride;
-};
-template <typename T, int ARRAYS>
-__device__ __forceinline__ void copy_tile(const Source<T> (&src)[ARRAYS], const ScanParams& p, int n, int chan0, int k0, int end, uint8_t* slot) {
-  constexpr int PER = 16 / (int)sizeof(T), COPIES = PIPE_CHANNELS / PER, ROUNDS = PIPE_STEPS * COPIES / PIPE_THREADS;
-  if (k0 >= end) return;
-#pragma unroll
-  for (int j = 0; j < ROUNDS; ++j) {
-    const int i = threadIdx.x + j * PIPE_THREADS, row = i / COPIES, c = i % COPIES * PER, k = k0 + row;
-    if (k < end && chan0 + c < p.C) {
-      const int t = p.reverse ? n - 1 - k : k;
-#pragma unroll
-      for (int a = 0; a < ARRAYS; ++a) {
-        const uint32_t dst = (uint32_t)__cvta_generic_to_shared(slot + ((a * PIPE_STEPS + row) * PIPE_CHANNELS + c) * sizeof(T));
-        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src[a].base + t * src[a].stride + c) : "memory");
-      }
-    }
+  static constexpr int PER = 16 / (int)sizeof(T), COPIES = PIPE_CHANNELS / PER, ROW_STEP = PIPE_THREADS / COPIES, ROUNDS = PIPE_STEPS / ROW_STEP;
+  const T* at;        // the thread's piece of the tile to be requested next
+  long long round;    // elements between rounds, in scan order
+  __device__ __forceinline__ void open(const void* base, long long offset, long long stride, const ScanParams& p, int n, int k0) {
+    const int k = k0 + (int)threadIdx.x / COPIES, c = (int)threadIdx.x % COPIES * PER;
+    at = reinterpret_cast<const T*>(base) + offset + c + (p.reverse ? n - 1 - k : k) * stride;
+    round = (p.reverse ? -stride : stride) * ROW_STEP;
   }
-}
+  // rows: how many of the tile's rows there are (for this thread: none, if its channels are not there)
+  __device__ __forceinline__ void request(uint8_t* slot, int rows) const {
+    const int row = (int)threadIdx.x / COPIES;
+    const uint32_t dst = (uint32_t)__cvta_generic_to_shared(slot + threadIdx.x * 16);
+#pragma unroll
+    for (int j = 0; j < ROUNDS; ++j)
+      if (row + j * ROW_STEP < rows)
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + j * PIPE_THREADS * 16), "l"(at + j * round) : "memory");
+  }
+  __device__ __forceinline__ void move(int tiles) { at += round * (ROUNDS * tiles); }
+};
 
 // The flag in front of step k0 + (lane & 7) of the warp's eight steps, as loaded; vote over the lanes 0 .. 7 to use it.
 __device__ __forceinline__ bool load_flag(const ScanParams& p, const uint8_t* done, int n, int k0, int lane) {
@@ -674,112 +667,131 @@ __device__ __forceinline__ float2 enter_chunk2(const ScanParams& p, PipeShared& 
   return carry;
 }
 
+// Eight steps of two channels; `cuts`: some step of the warp's has a cut in front of it.
+__device__ __forceinline__ bool cut_at(unsigned cut, int s) { return cut >> s & 1; }
+
 template <typename T, bool BLEND, bool CUT, bool AGG>
 __global__ void __launch_bounds__(PIPE_THREADS, PIPE_BLOCKS) scan_pipe_kernel(const __grid_constant__ ScanParams p) {
-  constexpr int SLOTS = PIPE_SLOTS<T>;
+  constexpr int SLOTS = PIPE_SLOTS<T>, S = PIPE_S;
   extern __shared__ __align__(16) uint8_t slots[];
   __shared__ PipeShared sh;
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int lane = threadIdx.x & 31, warp = __shfl_sync(~0u, threadIdx.x >> 5, 0);
   const int b = blockIdx.x / p.groups, group = blockIdx.x % p.groups, chan0 = group * PIPE_CHANNELS, c = chan0 + 2 * lane;
   const bool on = c < p.C;
   int n = p.length ? p.length[b] : p.L;
   n = n < 0 ? 0 : n > p.L ? p.L : n;
   const int first = blockIdx.y * p.chunk_len, end = min(n, first + p.chunk_len);
-  const Source<T> src[2] = {{reinterpret_cast<const T*>(p.g) + b * p.gb + chan0, p.gt}, {reinterpret_cast<const T*>(p.x) + b * p.xb + chan0, p.xt}};
+  Source<T> sg, sx;
+  sg.open(p.g, b * p.gb + chan0, p.gt, p, n, first);
+  sx.open(p.x, b * p.xb + chan0, p.xt, p, n, first);
+  const int there = chan0 + (int)threadIdx.x % Source<T>::COPIES * Source<T>::PER < p.C ? end : first;  // (rows this thread copies end here)
   const uint8_t* done = CUT ? p.done + (long long)b * p.L : nullptr;
-#pragma unroll
-  for (int s = 0; s < SLOTS - 1; ++s) {
-    copy_tile<T, 2>(src, p, n, chan0, first + s * PIPE_STEPS, end, slots + s * SLOT_BYTES<T, 2>);
+  auto request = [&](int k0, int slot) {
+    uint8_t* at = slots + slot * SLOT_BYTES<T, 2>;
+    sg.request(at, there - k0);
+    sx.request(at + SLOT_BYTES<T, 1>, there - k0);
+    sg.move(1);
+    sx.move(1);
     asm volatile("cp.async.commit_group;" ::: "memory");
-  }
+  };
+#pragma unroll
+  for (int s = 0; s < SLOTS - 1; ++s) request(first + s * PIPE_STEPS, s);
   float2 carry = make_float2(0.f, 0.f), product = make_float2(1.f, 1.f);
   bool any_cut = false;
   if (!AGG && on && p.h0) carry = pair_of(p.h0 + (long long)b * p.C + c);
   if (!AGG && p.chunks > 1 && first < n) carry = enter_chunk2<false>(p, sh, b, group, c, on, blockIdx.y, carry);
-  bool flag = CUT && load_flag(p, done, n, first + warp * PIPE_S, lane);
+  bool flag = CUT && load_flag(p, done, n, first + warp * S, lane);
   T* y = reinterpret_cast<T*>(p.y) + (long long)b * p.L * p.C + c;
+  const long long row = p.reverse ? -(long long)p.C : p.C;
+  T* out = y + (long long)(p.reverse ? n - 1 - first - warp * S : first + warp * S) * p.C;
+  float* kept = !AGG && p.states && on && warp == 0 ? p.states + ((long long)b * p.intervals + first / MARL_SCAN_INTERVAL) * p.C + c : nullptr;
   int slot = 0, par = 0;
   for (int k0 = first; k0 < end; k0 += PIPE_STEPS, par ^= 1) {
     asm volatile("cp.async.wait_group %0;" ::"n"(SLOTS - 2) : "memory");
     __syncthreads();
-    copy_tile<T, 2>(src, p, n, chan0, k0 + (SLOTS - 1) * PIPE_STEPS, end, slots + (slot == 0 ? SLOTS - 1 : slot - 1) * SLOT_BYTES<T, 2>);
-    asm volatile("cp.async.commit_group;" ::: "memory");
-    const int mine = k0 + warp * PIPE_S;
+    request(k0 + (SLOTS - 1) * PIPE_STEPS, slot == 0 ? SLOTS - 1 : slot - 1);
+    const int mine = k0 + warp * S;
     unsigned cut = 0;
     if (CUT) {
       cut = __ballot_sync(~0u, flag);
       flag = load_flag(p, done, n, mine + PIPE_STEPS, lane);
     }
-    const T* sg = reinterpret_cast<const T*>(slots + slot * SLOT_BYTES<T, 2>) + warp * PIPE_S * PIPE_CHANNELS + 2 * lane;
-    const T* sx = sg + PIPE_STEPS * PIPE_CHANNELS;
-    float2 a[PIPE_S], u[PIPE_S];
+    const T* tg = reinterpret_cast<const T*>(slots + slot * SLOT_BYTES<T, 2>) + warp * S * PIPE_CHANNELS + 2 * lane;
+    const T* tx = tg + PIPE_STEPS * PIPE_CHANNELS;
+    float2 a[S], u[S];
 #pragma unroll
-    for (int s = 0; s < PIPE_S; ++s) {
-      a[s] = pair_of(sg + s * PIPE_CHANNELS);
-      u[s] = pair_of(sx + s * PIPE_CHANNELS);
+    for (int s = 0; s < S; ++s) {
+      a[s] = pair_of(tg + s * PIPE_CHANNELS);
+      u[s] = pair_of(tx + s * PIPE_CHANNELS);
       if (BLEND) {
         float2 rest;
         gate_pair2(a[s], a[s], rest);
         u[s] = mul2(rest, u[s]);
       }
     }
-    if (mine + PIPE_S > end) {
+    const bool whole = mine + S <= end;
+    if (!whole) {
 #pragma unroll
-      for (int s = 0; s < PIPE_S; ++s)
+      for (int s = 0; s < S; ++s)
         if (mine + s >= end) {
           a[s] = make_float2(1.f, 1.f);
           u[s] = make_float2(0.f, 0.f);
         }
     }
     float2 A = a[0], H = u[0];
+#pragma unroll
+    for (int s = 1; s < S; ++s) A = mul2(A, a[s]);
     if (CUT && cut) {
 #pragma unroll
-      for (int s = 1; s < PIPE_S; ++s) {
-        H = apply2(a[s], u[s], cut >> s & 1, H);
-        A = mul2(A, a[s]);
-      }
+      for (int s = 1; s < S; ++s) H = apply2(a[s], u[s], cut_at(cut, s), H);
     } else {
 #pragma unroll
-      for (int s = 1; s < PIPE_S; ++s) {
-        H = fma2(a[s], H, u[s]);
-        A = mul2(A, a[s]);
-      }
+      for (int s = 1; s < S; ++s) H = fma2(a[s], H, u[s]);
     }
     sh.total[par][warp][lane] = make_float4(A.x, A.y, H.x, H.y);
     if (CUT && lane == 0) sh.cut[par][warp] = cut != 0;
     __syncthreads();
     const unsigned long long cuts = CUT ? *reinterpret_cast<const unsigned long long*>(sh.cut[par]) : 0ull;
     float2 enter = carry;
-    for (int i = 0; i < PIPE_WARPS; ++i) {
-      if (i == warp) enter = carry;
-      const float4 t = sh.total[par][i][lane];
-      const bool cu = CUT && (cuts >> (8 * i) & 1);
-      carry = apply2(make_float2(t.x, t.y), make_float2(t.z, t.w), cu, carry);
-      if (AGG) {
-        product = mul2(product, make_float2(t.x, t.y));
-        any_cut |= cu;
+    if (!CUT || cuts == 0) {
+#pragma unroll
+      for (int i = 0; i < PIPE_WARPS; ++i) {
+        const float4 t = sh.total[par][i][lane];
+        carry = fma2(make_float2(t.x, t.y), carry, make_float2(t.z, t.w));
+        if (i + 1 == warp) enter = carry;
+        if (AGG) product = mul2(product, make_float2(t.x, t.y));
       }
+    } else {
+      for (int i = 0; i < PIPE_WARPS; ++i) {
+        if (i == warp) enter = carry;
+        const float4 t = sh.total[par][i][lane];
+        carry = apply2(make_float2(t.x, t.y), make_float2(t.z, t.w), cuts >> (8 * i) & 1, carry);
+        if (AGG) product = mul2(product, make_float2(t.x, t.y));
+      }
+      any_cut = true;
     }
     if constexpr (!AGG) {
-      if (p.states && on && warp == 0) put_pair(p.states + ((long long)b * p.intervals + k0 / MARL_SCAN_INTERVAL) * p.C + c, enter);
+      if (kept) {
+        put_pair(kept, enter);
+        kept += p.C;
+      }
       if (on) {
-        const long long step = p.reverse ? -(long long)p.C : p.C;
-        T* at = y + (long long)(p.reverse ? n - 1 - mine : mine) * p.C;
         float2 h = enter;
-        if ((CUT && cut) || mine + PIPE_S > end) {
+        if (whole && !(CUT && cut)) {
 #pragma unroll
-          for (int s = 0; s < PIPE_S; ++s) {
-            h = apply2(a[s], u[s], CUT && (cut >> s & 1), h);
-            if (mine + s < end) put_pair(at + s * step, h);
+          for (int s = 0; s < S; ++s) {
+            h = fma2(a[s], h, u[s]);
+            put_pair(out + s * row, h);
           }
         } else {
 #pragma unroll
-          for (int s = 0; s < PIPE_S; ++s) {
-            h = fma2(a[s], h, u[s]);
-            put_pair(at + s * step, h);
+          for (int s = 0; s < S; ++s) {
+            h = apply2(a[s], u[s], CUT && cut_at(cut, s), h);
+            if (mine + s < end) put_pair(out + s * row, h);
           }
         }
       }
+      out += row * PIPE_STEPS;
     }
     slot = slot + 1 == SLOTS ? 0 : slot + 1;
   }
@@ -801,135 +813,168 @@ __global__ void __launch_bounds__(PIPE_THREADS, PIPE_BLOCKS) scan_pipe_kernel(co
 }
 
 template <typename T, bool BLEND, bool CUT, bool AGG>
-__global__ void __launch_bounds__(PIPE_THREADS, sizeof(T) == 4 ? 2 : PG) scan_pipe_grad_kernel(const __grid_constant__ ScanParams p) {
-  constexpr int SLOTS = PIPE_SLOTS<T>, ARRAYS = AGG ? 2 : 3;
+__global__ void __launch_bounds__(PIPE_THREADS, 2) scan_pipe_grad_kernel(const __grid_constant__ ScanParams p) {
+  constexpr int SLOTS = PIPE_SLOTS<T>, ARRAYS = AGG ? 2 : 3, S = PIPE_S;
   extern __shared__ __align__(16) uint8_t slots[];
   __shared__ PipeShared sh;
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int lane = threadIdx.x & 31, warp = __shfl_sync(~0u, threadIdx.x >> 5, 0);
   const int b = blockIdx.x / p.groups, group = blockIdx.x % p.groups, chan0 = group * PIPE_CHANNELS, c = chan0 + 2 * lane;
   const bool on = c < p.C;
   int n = p.length ? p.length[b] : p.L;
   n = n < 0 ? 0 : n > p.L ? p.L : n;
   const int first = blockIdx.y * p.chunk_len, end = min(n, first + p.chunk_len), used = (n + p.chunk_len - 1) / p.chunk_len;
-  Source<T> src[ARRAYS];
-  src[0] = {reinterpret_cast<const T*>(p.g) + b * p.gb + chan0, p.gt};
-  src[1] = {reinterpret_cast<const T*>(p.dy) + b * p.dyb + chan0, p.dyt};
-  if constexpr (!AGG) src[2] = {reinterpret_cast<const T*>(p.x) + b * p.xb + chan0, p.xt};
-  const uint8_t* done = CUT ? p.done + (long long)b * p.L : nullptr;
   const int tiles = first < end ? (end - first + PIPE_STEPS - 1) / PIPE_STEPS : 0;
-  auto request = [&](int tile, int into) {  // tiles are taken from the last to the first
-    if (tile >= 0) copy_tile<T, ARRAYS>(src, p, n, chan0, first + tile * PIPE_STEPS, end, slots + into * SLOT_BYTES<T, ARRAYS>);
+  const int last0 = first + (tiles - 1) * PIPE_STEPS;  // the tiles are taken from the last to the first
+  Source<T> sg, sd, sx;
+  sg.open(p.g, b * p.gb + chan0, p.gt, p, n, last0);
+  sd.open(p.dy, b * p.dyb + chan0, p.dyt, p, n, last0);
+  if (!AGG) sx.open(p.x, b * p.xb + chan0, p.xt, p, n, last0);
+  const int there = chan0 + (int)threadIdx.x % Source<T>::COPIES * Source<T>::PER < p.C ? end : first;
+  const uint8_t* done = CUT ? p.done + (long long)b * p.L : nullptr;
+  auto request = [&](int k0, int slot) {
+    if (k0 >= first) {
+      uint8_t* at = slots + slot * SLOT_BYTES<T, ARRAYS>;
+      sg.request(at, there - k0);
+      sd.request(at + SLOT_BYTES<T, 1>, there - k0);
+      sg.move(-1);
+      sd.move(-1);
+      if (!AGG) {
+        sx.request(at + SLOT_BYTES<T, 2>, there - k0);
+        sx.move(-1);
+      }
+    }
     asm volatile("cp.async.commit_group;" ::: "memory");
   };
 #pragma unroll
-  for (int s = 0; s < SLOTS - 1; ++s) request(tiles - 1 - s, s);
+  for (int s = 0; s < SLOTS - 1; ++s) request(last0 - s * PIPE_STEPS, s);
   const bool gone = CUT && !p.reverse && n > 0 && done[n - 1];
   float2 carry = make_float2(0.f, 0.f), product = make_float2(1.f, 1.f);
   bool any_cut = false;
   if (!AGG && on && p.dlast && !gone) carry = pair_of(p.dlast + (long long)b * p.C + c);
   if (!AGG && p.chunks > 1 && first < n) carry = enter_chunk2<true>(p, sh, b, group, c, on, used - 1 - (int)blockIdx.y, carry, used);
-  auto kept = [&](int k0) {
-    return !AGG && on && k0 >= first ? pair_of(p.states + ((long long)b * p.intervals + k0 / MARL_SCAN_INTERVAL) * p.C + c) : make_float2(0.f, 0.f);
-  };
-  const int last0 = first + (tiles - 1) * PIPE_STEPS;
-  bool flag = CUT && tiles && load_flag(p, done, n, last0 + warp * PIPE_S, lane);
-  float2 state = tiles ? kept(last0) : make_float2(0.f, 0.f);
+  const float* kept = p.states + ((long long)b * p.intervals + last0 / MARL_SCAN_INTERVAL) * p.C + c;
+  bool flag = CUT && tiles && load_flag(p, done, n, last0 + warp * S, lane);
+  float2 state = !AGG && tiles && on ? pair_of(kept) : make_float2(0.f, 0.f);
   T* dg = reinterpret_cast<T*>(p.dg) + (long long)b * p.L * p.C + c;
   T* dx = reinterpret_cast<T*>(p.dx) + (long long)b * p.L * p.C + c;
+  const long long row = p.reverse ? -(long long)p.C : p.C;
+  long long out = (long long)(p.reverse ? n - 1 - last0 - warp * S : last0 + warp * S) * p.C;
   int slot = 0, par = 0;
-  for (int i = tiles - 1; i >= 0; --i, par ^= 1) {
-    const int k0 = first + i * PIPE_STEPS, mine = k0 + warp * PIPE_S;
+  for (int k0 = last0; k0 >= first; k0 -= PIPE_STEPS, par ^= 1) {
+    const int mine = k0 + warp * S;
     asm volatile("cp.async.wait_group %0;" ::"n"(SLOTS - 2) : "memory");
     __syncthreads();
-    request(i - (SLOTS - 1), slot == 0 ? SLOTS - 1 : slot - 1);
+    request(k0 - (SLOTS - 1) * PIPE_STEPS, slot == 0 ? SLOTS - 1 : slot - 1);
     unsigned cut = 0;
-    if (CUT) {
-      cut = __ballot_sync(~0u, flag);
-      flag = i > 0 && load_flag(p, done, n, mine - PIPE_STEPS, lane);
-    }
     float2 enter = state;
-    if (i > 0) state = kept(k0 - PIPE_STEPS);
-    const T* sg = reinterpret_cast<const T*>(slots + slot * SLOT_BYTES<T, ARRAYS>) + warp * PIPE_S * PIPE_CHANNELS + 2 * lane;
-    const T *sd = sg + PIPE_STEPS * PIPE_CHANNELS, *sx = sd + PIPE_STEPS * PIPE_CHANNELS;
-    const bool full = mine + PIPE_S <= end;
-    // (dy and x of steps behind the end: the slot holds something older)
-    auto d_of = [&](int s) { return full || mine + s < end ? pair_of(sd + s * PIPE_CHANNELS) : make_float2(0.f, 0.f); };
-    auto x_of = [&](int s) { return full || mine + s < end ? pair_of(sx + s * PIPE_CHANNELS) : make_float2(0.f, 0.f); };
-    float2 a[PIPE_S], q[BLEND ? PIPE_S : 1];
-#pragma unroll
-    for (int s = 0; s < PIPE_S; ++s) {
-      a[s] = full || mine + s < end ? pair_of(sg + s * PIPE_CHANNELS) : make_float2(0.f, 0.f);
-      if (BLEND) gate_pair2(a[s], a[s], q[s]);
-      if (!full && mine + s >= end) a[s] = make_float2(1.f, 1.f);
+    if (CUT) cut = __ballot_sync(~0u, flag);
+    if (k0 > first) {
+      if (CUT) flag = load_flag(p, done, n, mine - PIPE_STEPS, lane);
+      kept -= p.C;
+      if (!AGG && on) state = pair_of(kept);
     }
-    float2 A = a[0], H = make_float2(0.f, 0.f), R = make_float2(0.f, 0.f);
+    const T* tg = reinterpret_cast<const T*>(slots + slot * SLOT_BYTES<T, ARRAYS>) + warp * S * PIPE_CHANNELS + 2 * lane;
+    const T *td = tg + PIPE_STEPS * PIPE_CHANNELS, *tx = td + PIPE_STEPS * PIPE_CHANNELS;
+    const bool plain = mine + S <= end && !(CUT && cut);
+    // PLAIN: all eight steps are there and nothing is cut.  (What a slot holds of steps behind the end is something older.)
+    float2 a[S], q[BLEND ? S : 1], A, H = make_float2(0.f, 0.f), R = make_float2(0.f, 0.f);
+    auto value = [&](auto tag, const T* t, int s) {
+      return decltype(tag)::value || mine + s < end ? pair_of(t + s * PIPE_CHANNELS) : make_float2(0.f, 0.f);
+    };
+    auto reduce = [&](auto tag) {
+      constexpr bool PLAIN = decltype(tag)::value;
 #pragma unroll
-    for (int s = 1; s < PIPE_S; ++s) A = mul2(A, a[s]);
-    if constexpr (!AGG) {
-#pragma unroll
-      for (int s = 0; s < PIPE_S; ++s) {
-        const float2 u = BLEND ? mul2(q[s], x_of(s)) : x_of(s);
-        H = apply2(a[s], u, CUT && (cut >> s & 1), H);
+      for (int s = 0; s < S; ++s) {
+        a[s] = value(tag, tg, s);
+        if (BLEND) gate_pair2(a[s], a[s], q[s]);
+        if (!PLAIN && mine + s >= end) a[s] = make_float2(1.f, 1.f);
       }
-    }
+      A = a[0];
 #pragma unroll
-    for (int s = PIPE_S - 1; s >= 0; --s) {
-      R = mul2(a[s], add2(d_of(s), R));
-      if (CUT && (cut >> s & 1)) R = make_float2(0.f, 0.f);
-    }
+      for (int s = 1; s < S; ++s) A = mul2(A, a[s]);
+      if constexpr (!AGG) {
+#pragma unroll
+        for (int s = 0; s < S; ++s) {
+          const float2 x = value(tag, tx, s), u = BLEND ? mul2(q[s], x) : x;
+          H = apply2(a[s], u, !PLAIN && cut_at(cut, s), H);
+        }
+      }
+#pragma unroll
+      for (int s = S - 1; s >= 0; --s) {
+        R = mul2(a[s], add2(value(tag, td, s), R));
+        if (!PLAIN && cut_at(cut, s)) R = make_float2(0.f, 0.f);
+      }
+    };
+    if (plain) reduce(std::true_type());
+    else reduce(std::false_type());
     sh.total[par][warp][lane] = make_float4(A.x, A.y, H.x, H.y);
     sh.back[par][warp][lane] = R;
     if (CUT && lane == 0) sh.cut[par][warp] = cut != 0;
     __syncthreads();
     const unsigned long long cuts = CUT ? *reinterpret_cast<const unsigned long long*>(sh.cut[par]) : 0ull;
-    if (!AGG)
-      for (int j = 0; j < warp; ++j) {
-        const float4 t = sh.total[par][j][lane];
-        enter = apply2(make_float2(t.x, t.y), make_float2(t.z, t.w), CUT && (cuts >> (8 * j) & 1), enter);
-      }
     float2 back = carry;
-    for (int j = PIPE_WARPS - 1; j >= 0; --j) {
-      if (j == warp) back = carry;
-      const float2 f = *reinterpret_cast<const float2*>(&sh.total[par][j][lane]);
-      const bool cu = CUT && (cuts >> (8 * j) & 1);
-      carry = apply2(f, sh.back[par][j][lane], cu, carry);
-      if (AGG) {
-        product = mul2(product, f);
-        any_cut |= cu;
+    if (!CUT || cuts == 0) {
+#pragma unroll
+      for (int j = 0; j < PIPE_WARPS - 1; ++j)
+        if (!AGG && j < warp) {
+          const float4 t = sh.total[par][j][lane];
+          enter = fma2(make_float2(t.x, t.y), enter, make_float2(t.z, t.w));
+        }
+#pragma unroll
+      for (int j = PIPE_WARPS - 1; j >= 0; --j) {
+        const float2 f = *reinterpret_cast<const float2*>(&sh.total[par][j][lane]);
+        carry = fma2(f, carry, sh.back[par][j][lane]);
+        if (j - 1 == warp) back = carry;
+        if (AGG) product = mul2(product, f);
       }
+    } else {
+      if (!AGG)
+        for (int j = 0; j < warp; ++j) {
+          const float4 t = sh.total[par][j][lane];
+          enter = apply2(make_float2(t.x, t.y), make_float2(t.z, t.w), cuts >> (8 * j) & 1, enter);
+        }
+      for (int j = PIPE_WARPS - 1; j >= 0; --j) {
+        if (j == warp) back = carry;
+        const float2 f = *reinterpret_cast<const float2*>(&sh.total[par][j][lane]);
+        carry = apply2(f, sh.back[par][j][lane], cuts >> (8 * j) & 1, carry);
+        if (AGG) product = mul2(product, f);
+      }
+      any_cut = true;
     }
     if constexpr (!AGG) {
-      if (on) {
-        const long long step = p.reverse ? -(long long)p.C : p.C;
-        const long long at = (long long)(p.reverse ? n - 1 - mine : mine) * p.C;
-        float2 G[PIPE_S];
+      auto emit = [&](auto tag) {
+        constexpr bool PLAIN = decltype(tag)::value;
+        float2 G[S];
 #pragma unroll
-        for (int s = PIPE_S - 1; s >= 0; --s) {
-          G[s] = add2(d_of(s), back);
+        for (int s = S - 1; s >= 0; --s) {
+          G[s] = add2(value(tag, td, s), back);
           back = mul2(a[s], G[s]);
-          if (CUT && (cut >> s & 1)) back = make_float2(0.f, 0.f);
+          if (!PLAIN && cut_at(cut, s)) back = make_float2(0.f, 0.f);
         }
         float2 h = enter;
+        T *og = dg + out, *ox = dx + out;
 #pragma unroll
-        for (int s = 0; s < PIPE_S; ++s) {
-          if (CUT && (cut >> s & 1)) h = make_float2(0.f, 0.f);
-          const float2 x = x_of(s);
-          float2 og, ox;
+        for (int s = 0; s < S; ++s) {
+          if (!PLAIN && cut_at(cut, s)) h = make_float2(0.f, 0.f);
+          const float2 x = value(tag, tx, s);
+          float2 vg, vx = G[s];
           if (BLEND) {
-            ox = mul2(G[s], q[s]);
-            og = mul2(add2(h, make_float2(-x.x, -x.y)), mul2(a[s], ox));
+            vx = mul2(G[s], q[s]);
+            vg = mul2(add2(h, make_float2(-x.x, -x.y)), mul2(a[s], vx));
             h = fma2(a[s], h, mul2(q[s], x));
           } else {
-            ox = G[s];
-            og = mul2(G[s], h);
+            vg = mul2(G[s], h);
             h = fma2(a[s], h, x);
           }
-          if (full || mine + s < end) {
-            put_pair(dg + at + s * step, og);
-            put_pair(dx + at + s * step, ox);
+          if (on && (PLAIN || mine + s < end)) {
+            put_pair(og + s * row, vg);
+            put_pair(ox + s * row, vx);
           }
         }
-      }
+      };
+      if (plain) emit(std::true_type());
+      else emit(std::false_type());
+      out -= row * PIPE_STEPS;
     }
     slot = slot + 1 == SLOTS ? 0 : slot + 1;
   }
