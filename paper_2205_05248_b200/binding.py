@@ -216,6 +216,11 @@ def _dptr(t):
 
 
 # ---- the learner's operators (device tensors, on the current stream of their device) ------------------------------------
+# Calls of a few microseconds of GPU work are common here, so the marshalling is kept short: no text is made unless a check
+# fails, the stream is asked for as a number, and dense outputs are made with their strides.
+_F32, _I32 = torch.float32, torch.int32
+
+
 def _need(ok: bool, text: str):
     if not ok:
         raise MarlError(text)
@@ -223,127 +228,149 @@ def _need(ok: bool, text: str):
 
 def _device_call(dev, fn, *args):
     """fn(stream, *args) with the tensors' device current, on its current stream."""
-    stream = C.c_void_p(torch.cuda.current_stream(dev).cuda_stream)
-    if torch.cuda.current_device() == dev.index:
-        _check(fn(stream, *args))
+    index = dev.index
+    stream = torch._C._cuda_getCurrentRawStream(index)
+    if torch._C._cuda_getDevice() == index:
+        rc = fn(stream, *args)
     else:
         with torch.cuda.device(dev):
-            _check(fn(stream, *args))
+            rc = fn(stream, *args)
+    if rc != 0:
+        _check(rc)
 
 
-def _same_device(dev, **tensors):
-    for name, t in tensors.items():
-        _need(t is None or t.device == dev, f"{name} is not on {dev}")
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+def _new(shape, dtype, dev):
+    """A dense tensor."""
+    stride, n = [], 1
+    for s in reversed(shape):
+        stride.append(n)
+        n *= s if s > 1 else 1
+    return torch.empty_strided(shape, stride[::-1], dtype=dtype, device=dev)
 
 
 def _rows_of(t, name: str):
     """t[..., A] as rows: (number of rows, elements between rows); the elements of a row must be neighbours."""
-    A = t.shape[-1]
-    _need(A >= 1, f"{name} has no entries")
-    _need(t.stride(-1) == 1 or A == 1, f"the entries of a row of {name} are not neighbours")
-    if t.numel() == 0:
-        return 0, A
-    if t.dim() == 2:
-        return t.shape[0], (t.stride(0) if t.shape[0] > 1 else A)
+    shape, strides = t.shape, t.stride()
+    A = shape[-1]
+    if A < 1 or (strides[-1] != 1 and A != 1):
+        raise MarlError(f"{name} has no entries, or the entries of a row are not neighbours")
     rows, stride = 1, None
-    for n, s in zip(reversed(t.shape[:-1]), reversed(t.stride()[:-1])):
+    for k in range(len(shape) - 2, -1, -1):
+        n = shape[k]
+        if n == 0:
+            return 0, A
         if n == 1:
             continue
         if stride is None:
-            stride = s
-        else:
-            _need(s == stride * rows, f"{name} cannot be walked as rows at one distance")
+            stride = strides[k]
+        elif strides[k] != stride * rows:
+            raise MarlError(f"{name} cannot be walked as rows at one distance")
         rows *= n
     return rows, (A if stride is None else stride)
 
 
-def _dense(t, dtype, shape, name: str):
+def _dense(t, dtype, shape, dev, name: str):
+    """The address of a dense tensor of that type and shape on that device; None for None."""
     if t is None:
         return None
-    _need(t.dtype == dtype, f"{name} must be {dtype}")
-    _need(tuple(t.shape) == tuple(shape), f"{name} must have shape {tuple(shape)}")
-    _need(t.is_contiguous(), f"{name} must be contiguous")
-    return t
+    if t.dtype is not dtype or t.shape != shape or t.device != dev or not t.is_contiguous():
+        raise MarlError(f"{name} must be a contiguous {dtype} tensor of shape {tuple(shape)} on {dev}")
+    return t.data_ptr()
 
 
 def _policy_rows(logits, action, avail, temperature: float):
-    _need(logits.is_cuda, "logits must be a CUDA tensor: there is no CPU path")
-    _need(logits.dtype in DTYPE, "logits must be float32, bfloat16 or float16")
-    _need(logits.dim() >= 1, "logits must have at least one dimension")
-    lead, A = tuple(logits.shape[:-1]), logits.shape[-1]
+    if not logits.is_cuda:
+        raise MarlError("logits must be a CUDA tensor: there is no CPU path")
+    dt = DTYPE.get(logits.dtype)
+    if dt is None or logits.dim() < 1:
+        raise MarlError("logits must be a float32, bfloat16 or float16 tensor of at least one dimension")
+    shape, dev = logits.shape, logits.device
+    lead = shape[:-1]
     rows, stride = _rows_of(logits, "logits")
-    _same_device(logits.device, action=action, avail=avail)
-    _dense(action, torch.int32, lead, "action")
-    astride = 0
+    if action is None:
+        raise MarlError("action is None")
+    act = _dense(action, _I32, lead, dev, "action")
+    av, astride = None, 0
     if avail is not None:
-        _need(avail.dtype in (torch.uint8, torch.bool) and tuple(avail.shape) == tuple(logits.shape),
-              "avail must be uint8 or bool of the logits' shape")
-        astride = _rows_of(avail, "avail")[1]
-    return lead, PolicyRows(_dptr(logits), _dptr(avail), _dptr(action), rows, stride, astride, A, DTYPE[logits.dtype],
-                            float(temperature), 0)
+        if avail.dtype not in (torch.uint8, torch.bool) or avail.shape != shape or avail.device != dev:
+            raise MarlError(f"avail must be a uint8 or bool tensor of shape {tuple(shape)} on {dev}")
+        av, astride = avail.data_ptr(), _rows_of(avail, "avail")[1]
+    return lead, dev, PolicyRows(logits.data_ptr(), av, act, rows, stride, astride, shape[-1], dt, temperature, 0)
 
 
 def marl_policy_logprob(logits, action, avail=None, temperature: float = 1.0, top: int = 0) -> dict:
     """Log probability of the action taken, entropy and the `top` best alternatives of each row of logits [..., A] (the q of a
     sampled batch).  action int32 [...], avail uint8 or bool [..., A].  Returns logp, entropy float32 [...], stats float32
     [..., 2] (for the gradient), top_index int32 and top_logp float32 [..., top] (None with top = 0)."""
-    lead, p = _policy_rows(logits, action, avail, temperature)
-    _need(0 <= top <= MAX_TOP, f"top must be in [0, {MAX_TOP}]")
-    f32 = dict(dtype=torch.float32, device=logits.device)
-    out = dict(logp=torch.empty(lead, **f32), entropy=torch.empty(lead, **f32), stats=torch.empty(lead + (2,), **f32),
-               top_index=None, top_logp=None)
+    lead, dev, p = _policy_rows(logits, action, avail, temperature)
+    if not 0 <= top <= MAX_TOP:
+        raise MarlError(f"top must be in [0, {MAX_TOP}]")
+    logp, entropy, stats = _new(lead, _F32, dev), _new(lead, _F32, dev), _new((*lead, 2), _F32, dev)
+    index = tops = None
     if top:
-        out["top_index"] = torch.empty(lead + (top,), dtype=torch.int32, device=logits.device)
-        out["top_logp"] = torch.empty(lead + (top,), **f32)
-    _device_call(logits.device, load_library().marl_policy_logprob, C.byref(p), C.c_int32(top), _dptr(out["logp"]),
-                 _dptr(out["entropy"]), _dptr(out["stats"]), _dptr(out["top_index"]), _dptr(out["top_logp"]))
-    return out
+        index, tops = _new((*lead, top), _I32, dev), _new((*lead, top), _F32, dev)
+    _device_call(dev, load_library().marl_policy_logprob, p, top, logp.data_ptr(), entropy.data_ptr(), stats.data_ptr(), _ptr(index),
+                 _ptr(tops))
+    return dict(logp=logp, entropy=entropy, stats=stats, top_index=index, top_logp=tops)
 
 
 def marl_policy_logprob_backward(logits, action, stats, entropy, g_logp=None, g_entropy=None, avail=None,
                                  temperature: float = 1.0, out=None):
     """The gradient of marl_policy_logprob with respect to the logits, from its stats and entropy and the gradients of logp and
-    entropy float32 [...] (either may be None).  Returns a tensor like logits (dense, or `out`, whose rows may be further apart)."""
-    lead, p = _policy_rows(logits, action, avail, temperature)
-    _same_device(logits.device, stats=stats, entropy=entropy, g_logp=g_logp, g_entropy=g_entropy, out=out)
-    _dense(stats, torch.float32, lead + (2,), "stats")
-    for name, t in (("entropy", entropy), ("g_logp", g_logp), ("g_entropy", g_entropy)):
-        _dense(t, torch.float32, lead, name)
+    entropy float32 [...] (either may be None).  Returns a tensor like logits (dense, or `out`, whose rows may be further apart; `out`
+    may be the logits)."""
+    lead, dev, p = _policy_rows(logits, action, avail, temperature)
+    if stats is None or entropy is None:
+        raise MarlError("stats or entropy is None")
+    st = _dense(stats, _F32, (*lead, 2), dev, "stats")
+    en, gl, ge = _dense(entropy, _F32, lead, dev, "entropy"), _dense(g_logp, _F32, lead, dev, "g_logp"), _dense(g_entropy, _F32, lead, dev, "g_entropy")
     if out is None:
-        out = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
-    _need(out.dtype == logits.dtype and out.shape == logits.shape, "out must be like logits")
-    _device_call(logits.device, load_library().marl_policy_logprob_backward, C.byref(p), _dptr(stats), _dptr(entropy),
-                 _dptr(g_logp), _dptr(g_entropy), _dptr(out), C.c_int64(_rows_of(out, "out")[1]))
+        out, stride = _new(logits.shape, logits.dtype, dev), logits.shape[-1]
+    else:
+        if out.dtype is not logits.dtype or out.shape != logits.shape or out.device != dev:
+            raise MarlError("out must be like logits")
+        stride = _rows_of(out, "out")[1]
+    _device_call(dev, load_library().marl_policy_logprob_backward, p, st, en, gl, ge, out.data_ptr(), stride)
     return out
 
 
 def _scan_args(gate, x, h0, done, length, form: str, reverse: bool):
-    _need(x.is_cuda, "x must be a CUDA tensor: there is no CPU path")
-    _need(x.dtype in DTYPE and gate.dtype == x.dtype, "gate and x must both be float32, bfloat16 or float16")
-    _need(x.dim() == 3 and gate.shape == x.shape, "gate and x must have the same shape [B, L, C]")
-    _need(form in SCAN_FORM, f"form must be one of {sorted(SCAN_FORM)}")
-    B, L, Cn = x.shape
-    _same_device(x.device, gate=gate, h0=h0, done=done, length=length)
-    _dense(h0, torch.float32, (B, Cn), "h0")
-    _dense(length, torch.int32, (B,), "length")
+    if not x.is_cuda:
+        raise MarlError("x must be a CUDA tensor: there is no CPU path")
+    dt, shape, dev = DTYPE.get(x.dtype), x.shape, x.device
+    if dt is None or gate.dtype is not x.dtype:
+        raise MarlError("gate and x must both be float32, bfloat16 or float16")
+    if len(shape) != 3 or gate.shape != shape or gate.device != dev:
+        raise MarlError("gate and x must have the same shape [B, L, C], on one device")
+    f = SCAN_FORM.get(form)
+    if f is None:
+        raise MarlError(f"form must be one of {sorted(SCAN_FORM)}")
+    B, L, Cn = shape
+    h, n = _dense(h0, _F32, (B, Cn), dev, "h0"), _dense(length, _I32, (B,), dev, "length")
+    d = None
     if done is not None:
-        _need(done.dtype in (torch.uint8, torch.bool), "done must be uint8 or bool")
-        _dense(done, done.dtype, (B, L), "done")
-    step = []
-    for name, t in (("gate", gate), ("x", x)):
-        c = t.stride(2) if Cn > 1 else 1
-        _need(c in (0, 1), f"the channels of {name} must be neighbours, or one value for all")
-        step.append((t.stride(0), t.stride(1), c))
-    (gb, gt, gc), (xb, xt, xc) = step
-    return Scan(_dptr(gate), _dptr(x), gb, gt, xb, xt, gc, xc, _dptr(h0), _dptr(done), _dptr(length), B, L, Cn, DTYPE[x.dtype],
-                SCAN_FORM[form], int(bool(reverse)))
+        d = _dense(done, torch.bool if done.dtype is torch.bool else torch.uint8, (B, L), dev, "done")
+    gb, gt, gc = gate.stride()
+    xb, xt, xc = x.stride()
+    if Cn <= 1:
+        gc = xc = 1
+    if gc not in (0, 1) or xc not in (0, 1):
+        raise MarlError("the channels of gate and of x must be neighbours, or one value for all")
+    return Scan(gate.data_ptr(), x.data_ptr(), gb, gt, xb, xt, gc, xc, h, d, n, B, L, Cn, dt, f, 1 if reverse else 0)
 
 
 def _scan_work(s, dev):
+    """Scratch of a call and its size (none where the time axis is short or the other axes are large, as most often)."""
+    if s.L <= SCAN_INTERVAL:
+        return None, 0
     need = C.c_size_t()
-    _check(load_library().marl_linear_scan_query(C.byref(s), None, C.byref(need)))
-    work = torch.empty(need.value, dtype=torch.uint8, device=dev) if need.value else None
-    return work, C.c_size_t(need.value)
+    _check(load_library().marl_linear_scan_query(s, None, need))
+    n = need.value
+    return (torch.empty(n, dtype=torch.uint8, device=dev) if n else None), n
 
 
 def marl_linear_scan(gate, x, h0=None, done=None, length=None, form: str = "blend", reverse: bool = False, keep: bool = False) -> dict:
@@ -351,15 +378,13 @@ def marl_linear_scan(gate, x, h0=None, done=None, length=None, form: str = "blen
     done uint8 or bool [B, L], length int32 [B], each may be None.  Returns y like x (dense), last float32 [B, C] and, with
     keep, the states that marl_linear_scan_backward takes."""
     s = _scan_args(gate, x, h0, done, length, form, reverse)
+    dev = x.device
     B, L, Cn = x.shape
-    out = dict(y=torch.empty((B, L, Cn), dtype=x.dtype, device=x.device),
-               last=torch.empty((B, Cn), dtype=torch.float32, device=x.device), states=None)
-    if keep:
-        out["states"] = torch.empty((B, -(-L // SCAN_INTERVAL), Cn), dtype=torch.float32, device=x.device)
-    work, need = _scan_work(s, x.device)
-    _device_call(x.device, load_library().marl_linear_scan, C.byref(s), _dptr(out["y"]), _dptr(out["last"]), _dptr(out["states"]),
-                 _dptr(work), need)
-    return out
+    y, last = _new((B, L, Cn), x.dtype, dev), _new((B, Cn), _F32, dev)
+    states = _new((B, -(-L // SCAN_INTERVAL), Cn), _F32, dev) if keep else None
+    work, need = _scan_work(s, dev)
+    _device_call(dev, load_library().marl_linear_scan, s, y.data_ptr(), last.data_ptr(), _ptr(states), _ptr(work), need)
+    return dict(y=y, last=last, states=states)
 
 
 def marl_linear_scan_backward(gate, x, states, dy, dlast=None, h0=None, done=None, length=None, form: str = "blend",
@@ -367,18 +392,19 @@ def marl_linear_scan_backward(gate, x, states, dy, dlast=None, h0=None, done=Non
     """The gradients of marl_linear_scan (called with the same arguments and keep=True) from those of y and, if not None, of last:
     dgate and dx like x (dense; the caller sums them where the inputs were expanded) and dh0 float32 [B, C]."""
     s = _scan_args(gate, x, h0, done, length, form, reverse)
+    dev = x.device
     B, L, Cn = x.shape
-    _same_device(x.device, states=states, dy=dy, dlast=dlast)
-    _dense(states, torch.float32, (B, -(-L // SCAN_INTERVAL), Cn), "states")
-    _dense(dlast, torch.float32, (B, Cn), "dlast")
-    _need(dy.dtype == x.dtype and dy.shape == x.shape, "dy must be like x")
-    _need(dy.stride(2) == 1 or Cn <= 1, "the channels of dy must be neighbours")
-    out = dict(dgate=torch.empty((B, L, Cn), dtype=x.dtype, device=x.device), dx=torch.empty((B, L, Cn), dtype=x.dtype, device=x.device),
-               dh0=torch.empty((B, Cn), dtype=torch.float32, device=x.device))
-    work, need = _scan_work(s, x.device)
-    _device_call(x.device, load_library().marl_linear_scan_backward, C.byref(s), _dptr(states), _dptr(dy), C.c_int64(dy.stride(0)),
-                 C.c_int64(dy.stride(1)), _dptr(dlast), _dptr(out["dgate"]), _dptr(out["dx"]), _dptr(out["dh0"]), _dptr(work), need)
-    return out
+    if states is None:
+        raise MarlError("states is None: call marl_linear_scan with keep=True")
+    st = _dense(states, _F32, (B, -(-L // SCAN_INTERVAL), Cn), dev, "states")
+    dl = _dense(dlast, _F32, (B, Cn), dev, "dlast")
+    if dy.dtype is not x.dtype or dy.shape != x.shape or dy.device != dev or (Cn > 1 and dy.stride(2) != 1):
+        raise MarlError("dy must be like x, its channels neighbours")
+    dgate, dx, dh0 = _new((B, L, Cn), x.dtype, dev), _new((B, L, Cn), x.dtype, dev), _new((B, Cn), _F32, dev)
+    work, need = _scan_work(s, dev)
+    _device_call(dev, load_library().marl_linear_scan_backward, s, st, dy.data_ptr(), dy.stride(0), dy.stride(1), dl, dgate.data_ptr(),
+                 dx.data_ptr(), dh0.data_ptr(), _ptr(work), need)
+    return dict(dgate=dgate, dx=dx, dh0=dh0)
 
 
 def marl_orthogonalise(mats, steps: int = 5, coeffs=(3.4445, -4.7750, 2.0315), eps: float = 1e-7, scale=1.0, out=None) -> list:
@@ -388,28 +414,31 @@ def marl_orthogonalise(mats, steps: int = 5, coeffs=(3.4445, -4.7750, 2.0315), e
     mats = list(mats)
     if not mats:
         return []
-    dev, dt = mats[0].device, mats[0].dtype
-    _need(mats[0].is_cuda, "matrices must be CUDA tensors: there is no CPU path")
-    _need(dt in DTYPE, "matrices must be float32, bfloat16 or float16")
-    _need(len(coeffs) == 3, "coeffs must be three numbers")
-    outs = [torch.empty(m.shape, dtype=dt, device=dev) for m in mats] if out is None else list(out)
-    scales = [float(s) for s in scale] if isinstance(scale, (list, tuple)) else [float(scale)] * len(mats)
-    _need(len(outs) == len(mats) == len(scales), "out and scale must be as long as the list")
-    arr = (Matrix * len(mats))()
-    for e, m, o, s in zip(arr, mats, outs, scales):
-        _need(m.dim() in (2, 3) and m.numel() > 0, "a matrix has shape [r, c] or [k, r, c]")
-        _need(m.device == dev and o.device == dev, "the matrices are not all on one device")
-        _need(m.dtype == dt and o.dtype == dt and o.shape == m.shape, "the matrices must share a dtype, and out must be like them")
-        for t in (m, o):
-            _need(t.stride(-1) == 1 or t.shape[-1] == 1, "the entries of a row must be neighbours")
-        e.in_, e.out, e.in_row, e.out_row = m.data_ptr(), o.data_ptr(), m.stride(-2), o.stride(-2)
-        if m.dim() == 3:
-            e.batch, e.in_batch, e.out_batch = m.shape[0], m.stride(0), o.stride(0)
+    dev, dtype = mats[0].device, mats[0].dtype
+    dt = DTYPE.get(dtype)
+    if not mats[0].is_cuda or dt is None:
+        raise MarlError("matrices must be float32, bfloat16 or float16 CUDA tensors: there is no CPU path")
+    if len(coeffs) != 3:
+        raise MarlError("coeffs must be three numbers")
+    outs = [_new(m.shape, dtype, dev) for m in mats] if out is None else list(out)
+    scales = scale if isinstance(scale, (list, tuple)) else [scale] * len(mats)
+    if not len(outs) == len(mats) == len(scales):
+        raise MarlError("out and scale must be as long as the list")
+    entries = []
+    for m, o, f in zip(mats, outs, scales):
+        shape = m.shape
+        if len(shape) not in (2, 3) or 0 in shape:
+            raise MarlError("a matrix has shape [r, c] or [k, r, c]")
+        if m.device != dev or o.device != dev or m.dtype is not dtype or o.dtype is not dtype or o.shape != shape:
+            raise MarlError("the matrices must share a device and a dtype, and out must be like them")
+        ms, os_ = m.stride(), o.stride()
+        if shape[-1] != 1 and (ms[-1] != 1 or os_[-1] != 1):
+            raise MarlError("the entries of a row must be neighbours")
+        if len(shape) == 3:
+            entries.append((m.data_ptr(), o.data_ptr(), ms[0], ms[1], os_[0], os_[1], shape[0], shape[1], shape[2], f))
         else:
-            e.batch = 1
-        e.rows, e.cols, e.scale = m.shape[-2], m.shape[-1], s
-    _device_call(dev, load_library().marl_orthogonalise, arr, C.c_int32(len(mats)), C.c_int32(DTYPE[dt]), C.c_int32(steps),
-                 (C.c_float * 3)(*coeffs), C.c_float(eps))
+            entries.append((m.data_ptr(), o.data_ptr(), 0, ms[0], 0, os_[0], 1, shape[0], shape[1], f))
+    _device_call(dev, load_library().marl_orthogonalise, (Matrix * len(entries))(*entries), len(entries), dt, steps, (C.c_float * 3)(*coeffs), eps)
     return outs
 
 

@@ -1087,8 +1087,17 @@ static int check_pointers(const marl_scan_t* in) {
   return MARL_OK;
 }
 
-static int set_work(ScanParams& p, void* work, size_t bytes) {
-  const size_t need = work_need(p);
+// What a caller has to bring, whatever the arrays' alignment turns out to be.
+static size_t work_wanted(const marl_scan_t* in) {
+  size_t need = work_need(scan_params(in, 1, false));
+  if (in->dtype != MARL_DTYPE_FP32) need = std::max(need, work_need(scan_params(in, 2, false)));
+  if (in->C >= 48 && in->L >= 32) need = std::max(need, work_need(scan_params(in, 2, true)));
+  return need;
+}
+
+static int set_work(ScanParams& p, const marl_scan_t* in, void* work, size_t bytes) {
+  if (in->L <= MARL_SCAN_INTERVAL) return MARL_OK;
+  const size_t need = work_wanted(in);
   if (!need) return MARL_OK;
   if (!work || bytes < need) return fail(MARL_ENOMEM, "work: %zu bytes given, %zu needed", work ? bytes : (size_t)0, need);
   if (misaligned(work, 16)) return fail(MARL_EALIGN, "work must be 16-byte aligned");
@@ -1184,10 +1193,7 @@ extern "C" int marl_linear_scan_query(const marl_scan_t* in, size_t* states_byte
   const int rc = check_scan(in);
   if (rc != MARL_OK) return rc;
   if (states_bytes) *states_bytes = (size_t)in->B * (((size_t)in->L + MARL_SCAN_INTERVAL - 1) / MARL_SCAN_INTERVAL) * in->C * 4;
-  if (work_bytes) {  // whatever the arrays' alignment turns out to be
-    const size_t one = work_need(scan_params(in, 1, false)), two = in->dtype == MARL_DTYPE_FP32 ? 0 : work_need(scan_params(in, 2, false));
-    *work_bytes = std::max(work_need(scan_params(in, 2, true)), std::max(one, two));
-  }
+  if (work_bytes) *work_bytes = in->L <= MARL_SCAN_INTERVAL ? 0 : work_wanted(in);
   return MARL_OK;
 }
 
@@ -1204,7 +1210,7 @@ extern "C" int marl_linear_scan(void* stream, const marl_scan_t* in, void* y, fl
   p.y = y;
   p.last = last;
   p.states = states;
-  if ((rc = set_work(p, work, work_bytes)) != MARL_OK) return rc;
+  if ((rc = set_work(p, in, work, work_bytes)) != MARL_OK) return rc;
   return dispatch(p, in->dtype, V, in->form == MARL_SCAN_BLEND, false, (cudaStream_t)stream);
 }
 
@@ -1232,6 +1238,6 @@ extern "C" int marl_linear_scan_backward(void* stream, const marl_scan_t* in, co
   p.dg = dgate;
   p.dx = dx;
   p.dh0 = dh0;
-  if ((rc = set_work(p, work, work_bytes)) != MARL_OK) return rc;
+  if ((rc = set_work(p, in, work, work_bytes)) != MARL_OK) return rc;
   return dispatch(p, in->dtype, V, in->form == MARL_SCAN_BLEND, true, (cudaStream_t)stream);
 }
