@@ -3,9 +3,11 @@
 // A matrix of up to 128 x 1024 (short side m, long side n) belongs to a cluster of 1 to 8 blocks and stays in its shared memory from the
 // load to the store: each block holds a slice of the long side, transposed (XT[j][i] = X[i][j], rows of the slice by
 // columns of the short side).  A step is
-//   each block's share of S from its slice                           -> all blocks add their rows of S up (in rank order)
-//   each block its rows of Q = c0 I + c1 S + c2 S S                   -> handed to all blocks
+//   each block's share of S from its slice, its rows sent to the blocks that own them
+//   each block the sum of the shares of its rows (in rank order), sent to all blocks
+//   each block its rows of Q = c0 I + c1 S + c2 S S, sent to all blocks
 //   each block XT <- XT Q on its slice, in place (a row of XT depends on that row alone)
+// Everything between blocks is sent, nothing fetched: stores into another block's shared memory are not waited for, loads from it are.
 // The products are plain fp32 multiply-adds with register tiles: the polynomial's slope at 0 amplifies rounding errors of
 // small singular directions (c0^5 = 485), so operands of fewer bits would show in the result.
 #include "learner_util.cuh"
@@ -32,18 +34,20 @@ struct OrthoGroup {
 };
 struct OrthoParams {
   OrthoGroup g[ORTHO_GROUPS];
-  int groups, steps;
+  int groups, steps, squares;
   float c0, c1, c2, eps;
 };
 
-// Floats of shared memory: the slice, S, and S's share or Q.
+// Floats of shared memory: the slice, the shares received, S, and Q.  Without room for the third square Q takes the place of the shares, and a
+// step ends with a barrier of the cluster.
 __host__ __device__ constexpr int padded_short(int m) { return m <= 16 ? 16 : m <= 32 ? 32 : m <= 64 ? 64 : 128; }
 __host__ __device__ constexpr int pitch_of(int mp) { return mp + 4; }  // rows start 16 bytes further round the banks
 __host__ __device__ inline int slice_of(int n, int cluster) { return ((n + cluster - 1) / cluster + 3) / 4 * 4; }
-inline size_t ortho_smem(int m, int n, int cluster) {
+inline size_t ortho_smem(int m, int n, int cluster, int squares) {
   const int mp = padded_short(m);
-  return 4 * ((size_t)slice_of(n, cluster) * pitch_of(mp) + 2 * (size_t)mp * mp);
+  return 4 * ((size_t)slice_of(n, cluster) * pitch_of(mp) + squares * (size_t)mp * mp);
 }
+constexpr size_t ORTHO_SMEM_MAX = 226 * 1024;
 
 // Columns of a 16-wide grid of threads: groups of four neighbours 64 apart where a thread has eight, so that a warp's 16-byte loads
 // meet every bank once.
@@ -99,8 +103,9 @@ __device__ void ortho_matrix(const OrthoParams& p, const OrthoGroup& g, int inde
   const int ns = slice_of(n, size), j0 = rank * ns;
   const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;
   float* xt = smem;                       // [ns][PITCH]
-  float* share = xt + ns * PITCH;         // [MP][MP] this block's share of S, then Q
-  float* s = share + MP * MP;             // [MP][MP]
+  float* shares = xt + ns * PITCH;        // [size][MP / size][MP] the blocks' shares of this block's rows of S
+  float* s = shares + MP * MP;            // [MP][MP]
+  float* qs = p.squares == 3 ? s + MP * MP : shares;
   __shared__ float exchange[2];           // largest modulus, sum of squares of the slice
   __shared__ float red[ORTHO_THREADS / 32];
 
@@ -177,13 +182,16 @@ __device__ void ortho_matrix(const OrthoParams& p, const OrthoGroup& g, int inde
           for (int j = 0; j < W; ++j) acc[i][j] = fmaf(a[i], b[j], acc[i][j]);
       }
 #pragma unroll
-      for (int i = 0; i < W; ++i) store_cols<W>(share + col_of<W>(ty, i) * MP, tx, acc[i]);
+      for (int i = 0; i < W; ++i) {
+        const int row = col_of<W>(ty, i), owner = row / rs;
+        store_cols<W>(cluster.map_shared_rank(shares, owner) + (rank * rs + row - owner * rs) * MP, tx, acc[i]);
+      }
     }
     cluster.sync();
     for (int i = tid; i < rs * MP / 4; i += ORTHO_THREADS) {
-      float4 t = make_float4(0.f, 0.f, 0.f, 0.f);
-      for (int r = 0; r < size; ++r) {
-        const float4 o = reinterpret_cast<const float4*>(cluster.map_shared_rank(share, r) + row0 * MP)[i];
+      float4 t = reinterpret_cast<const float4*>(shares)[i];
+      for (int r = 1; r < size; ++r) {
+        const float4 o = reinterpret_cast<const float4*>(shares + r * rs * MP)[i];
         t.x += o.x;
         t.y += o.y;
         t.z += o.z;
@@ -212,7 +220,7 @@ __device__ void ortho_matrix(const OrthoParams& p, const OrthoGroup& g, int inde
 #pragma unroll
             for (int j = 0; j < 4; ++j) q[j] = fmaf(p.c2, acc[i][j], p.c1 * e[j]) + (c + j == rows[i] ? p.c0 : 0.f);
             for (int o = 0; o < size; ++o)
-              *reinterpret_cast<float4*>(cluster.map_shared_rank(share, o) + rows[i] * MP + c) = make_float4(q[0], q[1], q[2], q[3]);
+              *reinterpret_cast<float4*>(cluster.map_shared_rank(qs, o) + rows[i] * MP + c) = make_float4(q[0], q[1], q[2], q[3]);
           }
         }
       };
@@ -222,33 +230,45 @@ __device__ void ortho_matrix(const OrthoParams& p, const OrthoGroup& g, int inde
     }
     cluster.sync();
     // XT <- XT Q: the 16 threads of a row are lanes of one warp, so a row is read by them all before any of them writes it
-    constexpr int R = 4;
-    for (int b = ty * R; b < ns; b += 16 * R) {
-      float acc[R][W];
+    auto times_q = [&](auto count) {
+      constexpr int R = decltype(count)::value;
+      for (int b = ty * R; b < ns; b += 16 * R) {
+        float acc[R][W];
+        const float* rows[R];
 #pragma unroll
-      for (int i = 0; i < R; ++i)
+        for (int i = 0; i < R; ++i) {
+          rows[i] = xt + min(b + i, ns - 1) * PITCH;
 #pragma unroll
-        for (int j = 0; j < W; ++j) acc[i][j] = 0.f;
-#pragma unroll 2
-      for (int k = 0; k < MP; k += 4) {
-        float a[R][4];
-#pragma unroll
-        for (int i = 0; i < R; ++i) *reinterpret_cast<float4*>(a[i]) = *reinterpret_cast<const float4*>(xt + (b + i) * PITCH + k);
-#pragma unroll
-        for (int kk = 0; kk < 4; ++kk) {
-          float q[W];
-          load_cols<W>(share + (k + kk) * MP, tx, q);
-#pragma unroll
-          for (int i = 0; i < R; ++i)
-#pragma unroll
-            for (int j = 0; j < W; ++j) acc[i][j] = fmaf(a[i][kk], q[j], acc[i][j]);
+          for (int j = 0; j < W; ++j) acc[i][j] = 0.f;
         }
-      }
-      __syncwarp(0xFFFFu << (tid & 16));
+#pragma unroll 2
+        for (int k = 0; k < MP; k += 4) {
+          float a[R][4];
 #pragma unroll
-      for (int i = 0; i < R; ++i) store_cols<W>(xt + (b + i) * PITCH, tx, acc[i]);
-    }
-    __syncthreads();
+          for (int i = 0; i < R; ++i) *reinterpret_cast<float4*>(a[i]) = *reinterpret_cast<const float4*>(rows[i] + k);
+#pragma unroll
+          for (int kk = 0; kk < 4; ++kk) {
+            float q[W];
+            load_cols<W>(qs + (k + kk) * MP, tx, q);
+#pragma unroll
+            for (int i = 0; i < R; ++i)
+#pragma unroll
+              for (int j = 0; j < W; ++j) acc[i][j] = fmaf(a[i][kk], q[j], acc[i][j]);
+          }
+        }
+        __syncwarp(0xFFFFu << (tid & 16));
+#pragma unroll
+        for (int i = 0; i < R; ++i)
+          if (b + i < ns) store_cols<W>(xt + (b + i) * PITCH, tx, acc[i]);
+        __syncwarp(0xFFFFu << (tid & 16));
+      }
+    };
+    if (ns > 48) times_q(std::integral_constant<int, 4>());
+    else if (ns > 32) times_q(std::integral_constant<int, 3>());
+    else if (ns > 16) times_q(std::integral_constant<int, 2>());
+    else times_q(std::integral_constant<int, 1>());
+    if (p.squares == 3) __syncthreads();
+    else cluster.sync();
   }
 
   T* out = reinterpret_cast<T*>(g.out) + (long long)index * g.out_batch;
@@ -340,19 +360,21 @@ extern "C" int marl_orthogonalise(void* stream, const marl_matrix_t* list, int32
       p.g[p.groups++] = OrthoGroup{g.in, g.out, g.in_batch, g.in_row, g.out_batch, g.out_row, (int)matrices, g.rows, g.cols, g.scale};
       matrices += g.batch;
     }
-    auto smem_for = [&](int cluster) {
+    auto smem_for = [&](int cluster, int squares) {
       size_t need = 0;
       for (int k = 0; k < p.groups; ++k)
-        need = std::max(need, ortho_smem(std::min(p.g[k].rows, p.g[k].cols), std::max(p.g[k].rows, p.g[k].cols), cluster));
+        need = std::max(need, ortho_smem(std::min(p.g[k].rows, p.g[k].cols), std::max(p.g[k].rows, p.g[k].cols), cluster, squares));
       return need;
     };
     i0 = i;
     if (p.groups == 0) continue;
     // Few matrices: as many blocks a matrix as the device has room for; more: as few as their shared memory allows.
+    p.squares = 3;
     int cluster = 1;
-    while (cluster < 8 && smem_for(cluster) > 200 * 1024) cluster *= 2;
+    while (cluster < 8 && smem_for(cluster, 3) > ORTHO_SMEM_MAX) cluster *= 2;
+    if (smem_for(cluster, 3) > ORTHO_SMEM_MAX) p.squares = 2;
     while (cluster < 8 && matrices * cluster * 2 <= ORTHO_SMS) cluster *= 2;
-    const size_t smem = smem_for(cluster);
+    const size_t smem = smem_for(cluster, p.squares);
     int rc;
     if (dtype == MARL_DTYPE_FP32) rc = launch_ortho<float>(p, (int)matrices, cluster, smem, 0, (cudaStream_t)stream);
     else if (dtype == MARL_DTYPE_BF16) rc = launch_ortho<__nv_bfloat16>(p, (int)matrices, cluster, smem, 1, (cudaStream_t)stream);
