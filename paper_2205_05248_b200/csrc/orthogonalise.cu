@@ -16,6 +16,7 @@
 #include <algorithm>
 #include <cmath>
 #include <cooperative_groups.h>
+#include <type_traits>
 
 namespace cg = cooperative_groups;
 
@@ -23,6 +24,9 @@ namespace marl {
 
 constexpr int ORTHO_THREADS = 256, ORTHO_GROUPS = 32;
 constexpr int ORTHO_SMS = 148;
+#ifndef CSMAX
+#define CSMAX 8
+#endif
 
 struct OrthoGroup {
   const void* in;
@@ -74,22 +78,24 @@ __device__ __forceinline__ void store_cols(float* row, int t, const float (&v)[W
   }
 }
 
-// out[r][c] = sum over k of a[k][r0 + r] a[k][c] for r < R of this thread's rows, four neighbouring columns.
-template <int MP, int R>
-__device__ __forceinline__ void square_rows(const float* a, const int (&rows)[R], int c, float (&acc)[R][4]) {
+// A tile of R x W elements of S S: rows r0 .. r0 + R - 1, this thread's columns, over k0 <= k < k1.  (S is symmetric: its rows are read.)
+template <int MP, int R, int W>
+__device__ __forceinline__ void square_tile(const float* s, int r0, int tx, int k0, int k1, float (&acc)[R][W]) {
 #pragma unroll
-  for (int r = 0; r < R; ++r) acc[r][0] = acc[r][1] = acc[r][2] = acc[r][3] = 0.f;
-#pragma unroll 8
-  for (int k = 0; k < MP; ++k) {
-    const float4 b = *reinterpret_cast<const float4*>(a + k * MP + c);
+  for (int r = 0; r < R; ++r)
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-      const float v = a[k * MP + rows[r]];
-      acc[r][0] = fmaf(v, b.x, acc[r][0]);
-      acc[r][1] = fmaf(v, b.y, acc[r][1]);
-      acc[r][2] = fmaf(v, b.z, acc[r][2]);
-      acc[r][3] = fmaf(v, b.w, acc[r][3]);
-    }
+    for (int j = 0; j < W; ++j) acc[r][j] = 0.f;
+#pragma unroll 4
+  for (int k = k0; k < k1; ++k) {
+    float a[R], b[W];
+    if constexpr (R == 4) *reinterpret_cast<float4*>(a) = *reinterpret_cast<const float4*>(s + k * MP + r0);
+    else if constexpr (R == 2) *reinterpret_cast<float2*>(a) = *reinterpret_cast<const float2*>(s + k * MP + r0);
+    else a[0] = s[k * MP + r0];
+    load_cols<W>(s + k * MP, tx, b);
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+#pragma unroll
+      for (int j = 0; j < W; ++j) acc[r][j] = fmaf(a[r], b[j], acc[r][j]);
   }
 }
 
@@ -200,33 +206,49 @@ __device__ void ortho_matrix(const OrthoParams& p, const OrthoGroup& g, int inde
       for (int r = 0; r < size; ++r) reinterpret_cast<float4*>(cluster.map_shared_rank(s, r) + row0 * MP)[i] = t;
     }
     cluster.sync();
-    {  // this block's rows of Q, to every block
-      constexpr int CG = MP / 4, RG = ORTHO_THREADS / CG;   // groups of four columns, threads along the rows
-      const int c = (tid % CG) * 4, r = tid / CG;
-      auto rows_of_q = [&](auto count) {
-        constexpr int R = decltype(count)::value;
-        for (int b = r; b < rs; b += RG * R) {
-          int rows[R];
-          float acc[R][4];
+    // This block's rows of S S, into `shares` (which is free now).  Tiles of R rows by MP / 16 columns keep the multiply-adds ahead of the
+    // loads; with few rows the threads that are left take parts of the sum over k, which are added up in their order.
+    auto square = [&](auto count) {
+      constexpr int R = decltype(count)::value;
+      const int bands = rs / R;                                  // of rows; 16 threads each
+      const int parts = bands >= 16 ? 1 : 16 / bands, len = MP / parts;
+      for (int b = ty % bands; b < bands; b += 16) {             // (ty / bands: which part)
+        const int part = bands >= 16 ? 0 : ty / bands;
+        float acc[R][W];
+        square_tile<MP, R, W>(s, row0 + b * R, tx, part * len, (part + 1) * len, acc);
 #pragma unroll
-          for (int i = 0; i < R; ++i) rows[i] = row0 + min(b + i * RG, rs - 1);
-          square_rows<MP, R>(s, rows, c, acc);
+        for (int r = 0; r < R; ++r) store_cols<W>(shares + (part * rs + b * R + r) * MP, tx, acc[r]);
+      }
+      return parts;
+    };
+    const int parts = square(std::integral_constant<int, W < 4 ? W : 4>());  // (parts * rs = 16 R <= MP rows of room)
+    __syncthreads();
+    // this block's rows of Q, to every block
+    float4 q[MP * MP / 4 / ORTHO_THREADS > 0 ? MP * MP / 4 / ORTHO_THREADS : 1];
+    int held = 0;
 #pragma unroll
-          for (int i = 0; i < R; ++i) {
-            if (b + i * RG >= rs) continue;
-            const float4 a = *reinterpret_cast<const float4*>(s + rows[i] * MP + c);
-            const float e[4] = {a.x, a.y, a.z, a.w};
-            float q[4];
+    for (int h = 0; h < (int)(sizeof(q) / sizeof(q[0])); ++h) {
+      const int i = tid + h * ORTHO_THREADS;
+      if (i >= rs * MP / 4) break;
+      float4 t = reinterpret_cast<const float4*>(shares)[i];
+      for (int r = 1; r < parts; ++r) {
+        const float4 o = reinterpret_cast<const float4*>(shares + r * rs * MP)[i];
+        t.x += o.x;
+        t.y += o.y;
+        t.z += o.z;
+        t.w += o.w;
+      }
+      const int row = row0 + i / (MP / 4), c = i % (MP / 4) * 4;
+      const float4 a = *reinterpret_cast<const float4*>(s + row * MP + c);
+      q[h] = make_float4(fmaf(p.c2, t.x, p.c1 * a.x) + (c == row ? p.c0 : 0.f), fmaf(p.c2, t.y, p.c1 * a.y) + (c + 1 == row ? p.c0 : 0.f),
+                         fmaf(p.c2, t.z, p.c1 * a.z) + (c + 2 == row ? p.c0 : 0.f), fmaf(p.c2, t.w, p.c1 * a.w) + (c + 3 == row ? p.c0 : 0.f));
+      held = h + 1;
+    }
+    if (p.squares != 3) cluster.sync();  // (Q takes the place of the parts, of every block)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) q[j] = fmaf(p.c2, acc[i][j], p.c1 * e[j]) + (c + j == rows[i] ? p.c0 : 0.f);
-            for (int o = 0; o < size; ++o)
-              *reinterpret_cast<float4*>(cluster.map_shared_rank(qs, o) + rows[i] * MP + c) = make_float4(q[0], q[1], q[2], q[3]);
-          }
-        }
-      };
-      if (rs >= 4 * RG) rows_of_q(std::integral_constant<int, 4>());
-      else if (rs >= 2 * RG) rows_of_q(std::integral_constant<int, 2>());
-      else rows_of_q(std::integral_constant<int, 1>());
+    for (int h = 0; h < (int)(sizeof(q) / sizeof(q[0])); ++h) {
+      if (h >= held) break;
+      for (int r = 0; r < size; ++r) reinterpret_cast<float4*>(cluster.map_shared_rank(qs, r) + row0 * MP)[tid + h * ORTHO_THREADS] = q[h];
     }
     cluster.sync();
     // XT <- XT Q: the 16 threads of a row are lanes of one warp, so a row is read by them all before any of them writes it
@@ -280,8 +302,9 @@ __device__ void ortho_matrix(const OrthoParams& p, const OrthoGroup& g, int inde
     }
 }
 
-template <typename T>
-__global__ void __launch_bounds__(ORTHO_THREADS, 1) orthogonalise_kernel(const __grid_constant__ OrthoParams p) {
+// MOST: the largest padded short side of the list.  Up to 64 two blocks share a multiprocessor.
+template <typename T, int MOST>
+__global__ void __launch_bounds__(ORTHO_THREADS, MOST == 128 ? 1 : 2) orthogonalise_kernel(const __grid_constant__ OrthoParams p) {
   extern __shared__ __align__(16) float ortho_smem_buf[];
   const int matrix = (int)(blockIdx.x / cg::this_cluster().num_blocks());
   int at = 0;
@@ -290,15 +313,15 @@ __global__ void __launch_bounds__(ORTHO_THREADS, 1) orthogonalise_kernel(const _
   const int m = min(g.rows, g.cols), index = matrix - g.first;
   if (m <= 16) ortho_matrix<T, 16>(p, g, index, ortho_smem_buf);
   else if (m <= 32) ortho_matrix<T, 32>(p, g, index, ortho_smem_buf);
-  else if (m <= 64) ortho_matrix<T, 64>(p, g, index, ortho_smem_buf);
-  else ortho_matrix<T, 128>(p, g, index, ortho_smem_buf);
+  else if (MOST == 64 || m <= 64) ortho_matrix<T, 64>(p, g, index, ortho_smem_buf);
+  else if constexpr (MOST == 128) ortho_matrix<T, 128>(p, g, index, ortho_smem_buf);
 }
 
-static uint32_t g_ortho_smem[3][SMEM_OPTIN_DEVICES];
+static uint32_t g_ortho_smem[6][SMEM_OPTIN_DEVICES];
 
-template <typename T>
+template <typename T, int MOST>
 static int launch_ortho(const OrthoParams& p, int matrices, int cluster, size_t smem, int which, cudaStream_t stream) {
-  auto* kernel = &orthogonalise_kernel<T>;
+  auto* kernel = &orthogonalise_kernel<T, MOST>;
   cudaError_t e = ensure_dynamic_smem(reinterpret_cast<const void*>(kernel), (uint32_t)smem, g_ortho_smem[which]);
   if (e != cudaSuccess) return fail(MARL_ECUDA, "marl_orthogonalise: %s", cudaGetErrorString(e));
   cudaLaunchConfig_t c = {};
@@ -373,12 +396,16 @@ extern "C" int marl_orthogonalise(void* stream, const marl_matrix_t* list, int32
     int cluster = 1;
     while (cluster < 8 && smem_for(cluster, 3) > ORTHO_SMEM_MAX) cluster *= 2;
     if (smem_for(cluster, 3) > ORTHO_SMEM_MAX) p.squares = 2;
-    while (cluster < 8 && matrices * cluster * 2 <= ORTHO_SMS) cluster *= 2;
+    while (cluster < CSMAX && matrices * cluster * 2 <= ORTHO_SMS) cluster *= 2;
     const size_t smem = smem_for(cluster, p.squares);
     int rc;
-    if (dtype == MARL_DTYPE_FP32) rc = launch_ortho<float>(p, (int)matrices, cluster, smem, 0, (cudaStream_t)stream);
-    else if (dtype == MARL_DTYPE_BF16) rc = launch_ortho<__nv_bfloat16>(p, (int)matrices, cluster, smem, 1, (cudaStream_t)stream);
-    else rc = launch_ortho<__half>(p, (int)matrices, cluster, smem, 2, (cudaStream_t)stream);
+    int most = 0;
+    for (int k = 0; k < p.groups; ++k) most = std::max(most, std::min(p.g[k].rows, p.g[k].cols));
+    rc = by_dtype(dtype, [&](auto t) {
+      using T = decltype(t);
+      return most <= 64 ? launch_ortho<T, 64>(p, (int)matrices, cluster, smem, dtype, (cudaStream_t)stream)
+                        : launch_ortho<T, 128>(p, (int)matrices, cluster, smem, dtype + 3, (cudaStream_t)stream);
+    });
     if (rc != MARL_OK) return rc;
   }
   return MARL_OK;
