@@ -22,11 +22,10 @@ namespace cg = cooperative_groups;
 
 namespace marl {
 
-constexpr int ORTHO_THREADS = 256, ORTHO_GROUPS = 32;
+// 256 threads: 16 matrices of hidden 128 in 115 us, the 256 of 64 hidden-64 networks in 143; with 512 threads for the former 129 us, with 128 for
+// the latter 174 us.
+constexpr int ORTHO_GROUPS = 32, ORTHO_THREADS = 256;
 constexpr int ORTHO_SMS = 148;
-#ifndef CSMAX
-#define CSMAX 8
-#endif
 
 struct OrthoGroup {
   const void* in;
@@ -78,6 +77,16 @@ __device__ __forceinline__ void store_cols(float* row, int t, const float (&v)[W
   }
 }
 
+// H neighbouring rows of a square, of one of its columns.
+template <int H>
+__device__ __forceinline__ void load_rows(const float* at, float (&v)[H]) {
+  if constexpr (H >= 4) {
+#pragma unroll
+    for (int i = 0; i < H; i += 4) *reinterpret_cast<float4*>(&v[i]) = *reinterpret_cast<const float4*>(at + i);
+  } else if constexpr (H == 2) *reinterpret_cast<float2*>(v) = *reinterpret_cast<const float2*>(at);
+  else v[0] = at[0];
+}
+
 // A tile of R x W elements of S S: rows r0 .. r0 + R - 1, this thread's columns, over k0 <= k < k1.  (S is symmetric: its rows are read.)
 template <int MP, int R, int W>
 __device__ __forceinline__ void square_tile(const float* s, int r0, int tx, int k0, int k1, float (&acc)[R][W]) {
@@ -88,9 +97,7 @@ __device__ __forceinline__ void square_tile(const float* s, int r0, int tx, int 
 #pragma unroll 4
   for (int k = k0; k < k1; ++k) {
     float a[R], b[W];
-    if constexpr (R == 4) *reinterpret_cast<float4*>(a) = *reinterpret_cast<const float4*>(s + k * MP + r0);
-    else if constexpr (R == 2) *reinterpret_cast<float2*>(a) = *reinterpret_cast<const float2*>(s + k * MP + r0);
-    else a[0] = s[k * MP + r0];
+    load_rows<R>(s + k * MP + r0, a);
     load_cols<W>(s + k * MP, tx, b);
 #pragma unroll
     for (int r = 0; r < R; ++r)
@@ -102,6 +109,8 @@ __device__ __forceinline__ void square_tile(const float* s, int r0, int tx, int 
 template <typename T, int MP>
 __device__ void ortho_matrix(const OrthoParams& p, const OrthoGroup& g, int index, float* smem) {
   constexpr int PITCH = pitch_of(MP), W = MP / 16;
+  // The threads form a grid of 16 columns (W columns of a square each) by ORTHO_THREADS / 16 rows, of which the first TY have H rows of a square each.
+  constexpr int ROWS = ORTHO_THREADS / 16, TY = ROWS < MP ? ROWS : MP, H = MP / TY;
   cg::cluster_group cluster = cg::this_cluster();
   const int rank = (int)cluster.block_rank(), size = (int)cluster.num_blocks();
   const bool tall = g.rows > g.cols;
@@ -172,25 +181,27 @@ __device__ void ortho_matrix(const OrthoParams& p, const OrthoGroup& g, int inde
   const int rs = MP / size, row0 = rank * rs;    // this block's rows of S and Q
   for (int step = 0; step < p.steps; ++step) {
     {  // this block's share of S
-      float acc[W][W];
+      float acc[H][W];
 #pragma unroll
-      for (int i = 0; i < W; ++i)
+      for (int i = 0; i < H; ++i)
 #pragma unroll
         for (int j = 0; j < W; ++j) acc[i][j] = 0.f;
+      if (ty < TY) {
 #pragma unroll 4
-      for (int k = 0; k < ns; ++k) {
-        float a[W], b[W];
-        load_cols<W>(xt + k * PITCH, ty, a);
-        load_cols<W>(xt + k * PITCH, tx, b);
+        for (int k = 0; k < ns; ++k) {
+          float a[H], b[W];
+          load_rows<H>(xt + k * PITCH + ty * H, a);
+          load_cols<W>(xt + k * PITCH, tx, b);
 #pragma unroll
-        for (int i = 0; i < W; ++i)
+          for (int i = 0; i < H; ++i)
 #pragma unroll
-          for (int j = 0; j < W; ++j) acc[i][j] = fmaf(a[i], b[j], acc[i][j]);
-      }
+            for (int j = 0; j < W; ++j) acc[i][j] = fmaf(a[i], b[j], acc[i][j]);
+        }
 #pragma unroll
-      for (int i = 0; i < W; ++i) {
-        const int row = col_of<W>(ty, i), owner = row / rs;
-        store_cols<W>(cluster.map_shared_rank(shares, owner) + (rank * rs + row - owner * rs) * MP, tx, acc[i]);
+        for (int i = 0; i < H; ++i) {
+          const int row = ty * H + i, owner = row / rs;
+          store_cols<W>(cluster.map_shared_rank(shares, owner) + (rank * rs + row - owner * rs) * MP, tx, acc[i]);
+        }
       }
     }
     cluster.sync();
@@ -208,20 +219,21 @@ __device__ void ortho_matrix(const OrthoParams& p, const OrthoGroup& g, int inde
     cluster.sync();
     // This block's rows of S S, into `shares` (which is free now).  Tiles of R rows by MP / 16 columns keep the multiply-adds ahead of the
     // loads; with few rows the threads that are left take parts of the sum over k, which are added up in their order.
-    auto square = [&](auto count) {
-      constexpr int R = decltype(count)::value;
-      const int bands = rs / R;                                  // of rows; 16 threads each
-      const int parts = bands >= 16 ? 1 : 16 / bands, len = MP / parts;
-      for (int b = ty % bands; b < bands; b += 16) {             // (ty / bands: which part)
-        const int part = bands >= 16 ? 0 : ty / bands;
-        float acc[R][W];
-        square_tile<MP, R, W>(s, row0 + b * R, tx, part * len, (part + 1) * len, acc);
+    int parts;
+    {
+      constexpr int R = H < 4 ? H : 4;
+      const int bands = rs / R;                     // of rows; 16 threads each
+      parts = bands >= TY ? 1 : TY / bands;         // (parts * rs <= MP rows of room)
+      const int len = MP / parts;
+      if (ty < TY && bands > 0)
+        for (int b = ty % bands; b < bands; b += TY) {  // (ty / bands: which part)
+          const int part = bands >= TY ? 0 : ty / bands;
+          float acc[R][W];
+          square_tile<MP, R, W>(s, row0 + b * R, tx, part * len, (part + 1) * len, acc);
 #pragma unroll
-        for (int r = 0; r < R; ++r) store_cols<W>(shares + (part * rs + b * R + r) * MP, tx, acc[r]);
-      }
-      return parts;
-    };
-    const int parts = square(std::integral_constant<int, W < 4 ? W : 4>());  // (parts * rs = 16 R <= MP rows of room)
+          for (int r = 0; r < R; ++r) store_cols<W>(shares + (part * rs + b * R + r) * MP, tx, acc[r]);
+        }
+    }
     __syncthreads();
     // this block's rows of Q, to every block
     float4 q[MP * MP / 4 / ORTHO_THREADS > 0 ? MP * MP / 4 / ORTHO_THREADS : 1];
@@ -254,7 +266,7 @@ __device__ void ortho_matrix(const OrthoParams& p, const OrthoGroup& g, int inde
     // XT <- XT Q: the 16 threads of a row are lanes of one warp, so a row is read by them all before any of them writes it
     auto times_q = [&](auto count) {
       constexpr int R = decltype(count)::value;
-      for (int b = ty * R; b < ns; b += 16 * R) {
+      for (int b = ty * R; b < ns; b += ROWS * R) {
         float acc[R][W];
         const float* rows[R];
 #pragma unroll
@@ -285,9 +297,9 @@ __device__ void ortho_matrix(const OrthoParams& p, const OrthoGroup& g, int inde
         __syncwarp(0xFFFFu << (tid & 16));
       }
     };
-    if (ns > 48) times_q(std::integral_constant<int, 4>());
-    else if (ns > 32) times_q(std::integral_constant<int, 3>());
-    else if (ns > 16) times_q(std::integral_constant<int, 2>());
+    if (ns > 3 * ROWS) times_q(std::integral_constant<int, 4>());
+    else if (ns > 2 * ROWS) times_q(std::integral_constant<int, 3>());
+    else if (ns > ROWS) times_q(std::integral_constant<int, 2>());
     else times_q(std::integral_constant<int, 1>());
     if (p.squares == 3) __syncthreads();
     else cluster.sync();
@@ -396,7 +408,7 @@ extern "C" int marl_orthogonalise(void* stream, const marl_matrix_t* list, int32
     int cluster = 1;
     while (cluster < 8 && smem_for(cluster, 3) > ORTHO_SMEM_MAX) cluster *= 2;
     if (smem_for(cluster, 3) > ORTHO_SMEM_MAX) p.squares = 2;
-    while (cluster < CSMAX && matrices * cluster * 2 <= ORTHO_SMS) cluster *= 2;
+    while (cluster < 8 && matrices * cluster * 2 <= ORTHO_SMS) cluster *= 2;
     const size_t smem = smem_for(cluster, p.squares);
     int rc;
     int most = 0;
