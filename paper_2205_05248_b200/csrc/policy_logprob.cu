@@ -255,22 +255,23 @@ __device__ __forceinline__ uint32_t prmt(uint32_t a, uint32_t sel) {
 // The highest bit of each byte, set where the byte is not 0.
 __device__ __forceinline__ uint32_t nonzero_bytes(uint32_t w) { return ((w & 0x7F7F7F7Fu) + 0x7F7F7F7Fu) | w; }
 
-// FLOOR: what values are raised to (-2^100; for fp16 its lowest number).
+// FLOOR: what values are raised to (-2^100; for fp16 its lowest number).  hide<BITS>: unavailable entries become BITS.
 template <typename T> struct Vec;
 template <> struct Vec<float> {
   static constexpr int N = 4;
-  static constexpr uint32_t FLOOR_BITS = 0xF1800000u;
+  static constexpr uint32_t FLOOR_BITS = 0xF1800000u, NEG_INF_BITS = 0xFF800000u;
   static __device__ __forceinline__ float floor_value() { return __uint_as_float(FLOOR_BITS); }
   static __device__ __forceinline__ void unpack(const uint4& r, float (&v)[4]) {
     v[0] = __uint_as_float(r.x); v[1] = __uint_as_float(r.y); v[2] = __uint_as_float(r.z); v[3] = __uint_as_float(r.w);
   }
+  template <uint32_t F>
   static __device__ __forceinline__ void hide(uint4& r, const uint32_t (&w)[1]) {
     const uint32_t t = nonzero_bytes(w[0]);
     const uint32_t a = prmt(t, 0x8888), b = prmt(t, 0x9999), c = prmt(t, 0xAAAA), d = prmt(t, 0xBBBB);
-    r.x = (r.x & a) | (FLOOR_BITS & ~a);
-    r.y = (r.y & b) | (FLOOR_BITS & ~b);
-    r.z = (r.z & c) | (FLOOR_BITS & ~c);
-    r.w = (r.w & d) | (FLOOR_BITS & ~d);
+    r.x = (r.x & a) | (F & ~a);
+    r.y = (r.y & b) | (F & ~b);
+    r.z = (r.z & c) | (F & ~c);
+    r.w = (r.w & d) | (F & ~d);
   }
   static __device__ __forceinline__ uint32_t raise(uint32_t w) { return __float_as_uint(max_nan(__uint_as_float(w), floor_value())); }
   static __device__ __forceinline__ float largest(const uint4& r) {
@@ -279,8 +280,8 @@ template <> struct Vec<float> {
 };
 template <typename T> struct Vec16 {
   static constexpr int N = 8;
+  template <uint32_t F>
   static __device__ __forceinline__ void hide(uint4& r, const uint32_t (&w)[2]) {
-    constexpr uint32_t F = Vec<T>::FLOOR_BITS;
     const uint32_t t = nonzero_bytes(w[0]), u = nonzero_bytes(w[1]);
     const uint32_t a = prmt(t, 0x9988), b = prmt(t, 0xBBAA), c = prmt(u, 0x9988), d = prmt(u, 0xBBAA);
     r.x = (r.x & a) | (F & ~a);
@@ -302,7 +303,7 @@ template <typename T> struct Vec16 {
   }
 };
 template <> struct Vec<__nv_bfloat16> : Vec16<__nv_bfloat16> {
-  static constexpr uint32_t FLOOR_BITS = 0xF180F180u;
+  static constexpr uint32_t FLOOR_BITS = 0xF180F180u, NEG_INF_BITS = 0xFF80FF80u;
   static __device__ __forceinline__ float floor_value() { return __uint_as_float(0xF1800000u); }
   static __device__ __forceinline__ uint32_t max2(uint32_t a, uint32_t b) {
     uint32_t r;
@@ -315,7 +316,7 @@ template <> struct Vec<__nv_bfloat16> : Vec16<__nv_bfloat16> {
   }
 };
 template <> struct Vec<__half> : Vec16<__half> {
-  static constexpr uint32_t FLOOR_BITS = 0xFBFFFBFFu;
+  static constexpr uint32_t FLOOR_BITS = 0xFBFFFBFFu, NEG_INF_BITS = 0xFC00FC00u;
   static __device__ __forceinline__ float floor_value() { return -65504.f; }
   static __device__ __forceinline__ uint32_t max2(uint32_t a, uint32_t b) {
     uint32_t r;
@@ -444,20 +445,19 @@ struct Row {
     if (MASK) {
       uint32_t w[N / 4];
       load_avail<N>(av + head + i * N, w);
-      Vec<T>::hide(r, w);
+      Vec<T>::template hide<Vec<T>::FLOOR_BITS>(r, w);
     }
     return r;
   }
   // vector i with its unavailable entries at -infinity
   __device__ __forceinline__ void values(int i, float (&v)[N]) const {
-    Vec<T>::unpack(__ldg(vectors() + i), v);
+    uint4 r = __ldg(vectors() + i);
     if (MASK) {
       uint32_t w[N / 4];
       load_avail<N>(av + head + i * N, w);
-#pragma unroll
-      for (int j = 0; j < N; ++j)
-        if (!(w[j / 4] >> (8 * (j & 3)) & 0xFF)) v[j] = -INFINITY;
+      Vec<T>::template hide<Vec<T>::NEG_INF_BITS>(r, w);
     }
+    Vec<T>::unpack(r, v);
   }
 };
 
@@ -710,6 +710,33 @@ template <typename T> struct Four16 {
 template <> struct Four<__nv_bfloat16> : Four16<__nv_bfloat16> {};
 template <> struct Four<__half> : Four16<__half> {};
 
+// Batcher's odd-even merge sort of a thread's numbers, descending; all indexes are constants, so that they stay in registers.
+template <int LO, int LEN, int STEP, int N>
+__device__ __forceinline__ void merge_halves(int (&a)[N]) {
+  if constexpr (2 * STEP < LEN) {
+    merge_halves<LO, LEN, 2 * STEP>(a);
+    merge_halves<LO + STEP, LEN, 2 * STEP>(a);
+#pragma unroll
+    for (int i = LO + STEP; i + STEP < LO + LEN; i += 2 * STEP) {
+      const int hi = max(a[i], a[i + STEP]), lo = min(a[i], a[i + STEP]);
+      a[i] = hi;
+      a[i + STEP] = lo;
+    }
+  } else {
+    const int hi = max(a[LO], a[LO + STEP]), lo = min(a[LO], a[LO + STEP]);
+    a[LO] = hi;
+    a[LO + STEP] = lo;
+  }
+}
+template <int LO, int LEN, int N>
+__device__ __forceinline__ void sort_descending(int (&a)[N]) {
+  if constexpr (LEN > 1) {
+    sort_descending<LO, LEN / 2>(a);
+    sort_descending<LO + LEN / 2, LEN / 2>(a);
+    merge_halves<LO, LEN, 1>(a);
+  }
+}
+
 template <typename T, int MA, bool DENSE>
 __global__ void __launch_bounds__(SMALL_ROWS) logprob_small_kernel(const __grid_constant__ RowsParams p, uint32_t inv_a) {
   __shared__ float xs[SMALL_ROWS * (MA + 1)];
@@ -774,42 +801,70 @@ __global__ void __launch_bounds__(SMALL_ROWS) logprob_small_kernel(const __grid_
   const bool has = act >= 0 && act < A;
   const float ls = write_row(p, row, a, has, has ? mine[act] : -INFINITY);
   if (!p.top) return;
-  if (m != m) {  // a NaN ranks above all numbers: +infinity in its place, and that below it
+  // Keys that order like the values with their five lowest bits replaced by the index: one sort ranks them all, exactly where those bits
+  // are 0 (16-bit types) and nearly always in fp32; where two neighbours come out the wrong way round, and with NaN, one by one.
+  int key[MA];
 #pragma unroll
-    for (int j = 0; j < MA; ++j) v[j] = v[j] != v[j] ? INFINITY : v[j] == INFINITY ? 3.402823466e38f : v[j];
+  for (int j = 0; j < MA; ++j) {
+    const int b = __float_as_int(v[j] + 0.0f);
+    key[j] = ((b ^ ((b >> 31) & 0x7FFFFFFF)) & ~31) | (31 - j);
   }
-  int out_j[4];
-  float out_l[4];
-  for (int k0 = 0; k0 < p.top; k0 += 4) {
+  sort_descending<0, MA>(key);
+  bool exact = m == m;
+  float before = INFINITY;
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      float top = -INFINITY;
-      int bj = -1;
+  for (int k = 0; k < MA; ++k)
+    if (k <= p.top) {
+      const int j = 31 - (key[k] & 31);
+      const float x = j < A ? mine[j] : -INFINITY;
+      exact = exact && x <= before;
+      before = x;
+    }
+  int* ti = p.top_index + row * p.top;
+  float* tl = p.top_logp + row * p.top;
+  if (exact) {
 #pragma unroll
-      for (int j = 0; j < MA; ++j)
-        if (v[j] > top) {
-          top = v[j];
+    for (int k0 = 0; k0 < MA; k0 += 4) {
+      if (k0 >= p.top) break;
+      int out_j[4];
+      float out_l[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int j = 31 - (key[k0 + k] & 31);
+        const float x = j < A ? mine[j] : -INFINITY;
+        out_j[k] = x == -INFINITY ? -1 : j;
+        out_l[k] = x == -INFINITY ? -INFINITY : (x - a.m) * p.it - ls;
+      }
+      if (p.fours) {
+        *reinterpret_cast<int4*>(ti + k0) = *reinterpret_cast<int4*>(out_j);
+        *reinterpret_cast<float4*>(tl + k0) = *reinterpret_cast<float4*>(out_l);
+      } else {
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          if (k0 + k < p.top) {
+            ti[k0 + k] = out_j[k];
+            tl[k0 + k] = out_l[k];
+          }
+      }
+    }
+    for (int k = MA; k < p.top; ++k) {
+      ti[k] = -1;
+      tl[k] = -INFINITY;
+    }
+  } else {
+    unsigned used = 0;
+    for (int k = 0; k < p.top; ++k) {
+      int bk = KEY_NEG_INF, bj = -1;
+      for (int j = 0; j < A; ++j) {
+        const int o = order_key(mine[j]);
+        if (o > bk && !(used >> j & 1)) {
+          bk = o;
           bj = j;
         }
-#pragma unroll
-      for (int j = 0; j < MA; ++j)
-        if (j == bj) v[j] = -INFINITY;
-      out_j[k] = bj;
-      out_l[k] = bj >= 0 ? (mine[bj] - a.m) * p.it - ls : -INFINITY;
-      if (k0 + k + 1 >= p.top) break;
-    }
-    int* ti = p.top_index + row * p.top + k0;
-    float* tl = p.top_logp + row * p.top + k0;
-    if (p.fours) {
-      *reinterpret_cast<int4*>(ti) = *reinterpret_cast<int4*>(out_j);
-      *reinterpret_cast<float4*>(tl) = *reinterpret_cast<float4*>(out_l);
-    } else {
-#pragma unroll
-      for (int k = 0; k < 4; ++k)
-        if (k0 + k < p.top) {
-          ti[k] = out_j[k];
-          tl[k] = out_l[k];
-        }
+      }
+      used |= bj >= 0 ? 1u << bj : 0u;
+      ti[k] = bj;
+      tl[k] = bj >= 0 ? (mine[bj] - a.m) * p.it - ls : -INFINITY;
     }
   }
 }
@@ -843,11 +898,18 @@ __device__ __forceinline__ float entry_grad(float m, float ls2, float k, float h
   return -ex2(l) * fmaf(h, l, k);
 }
 
+// Two of them, in packed arithmetic; c2 = (c, c), m2 = -(m, m) and so on.
+__device__ __forceinline__ float2 entry_grad2(float2 m2, float2 c2, float2 ls2, float2 k2, float2 h2, float x0, float x1) {
+  float2 l = fma2(add2(make_float2(x0, x1), m2), c2, ls2);
+  l = make_float2(max_nan(l.x, -200.f), max_nan(l.y, -200.f));
+  return mul2(make_float2(ex2(l.x), ex2(l.y)), fma2(h2, l, k2));
+}
+
 // A warp per segment of a row of more than SMALL_A actions, 16 bytes of the gradient a lane.  Where the logits' rows lie otherwise than the
 // gradient's from a 16-byte boundary, each lane takes its logits from the two aligned vectors that hold them, the second from the
 // lane behind it.
 template <typename T, bool MASK>
-__global__ void __launch_bounds__(256) logprob_wide_grad_kernel(const __grid_constant__ RowsGradParams q) {
+__global__ void __launch_bounds__(256, 4) logprob_wide_grad_kernel(const __grid_constant__ RowsGradParams q) {
   constexpr int N = Vec<T>::N;
   const int lane = threadIdx.x & 31;
   const long long unit = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
@@ -882,6 +944,8 @@ __global__ void __launch_bounds__(256) logprob_wide_grad_kernel(const __grid_con
   };
   fetch(i0);
   const RowGrad g = row_grad(q, row);
+  const float2 m2 = make_float2(-g.m, -g.m), c2 = make_float2(c, c), ls2 = make_float2(-g.ls2, -g.ls2), k2 = make_float2(-g.k, -g.k),
+               h2 = make_float2(-g.h, -g.h);
   auto single = [&](int j) {
     float v = to_f32(x[j]);
     if (MASK && !av[j]) v = -INFINITY;
@@ -923,15 +987,15 @@ __global__ void __launch_bounds__(256) logprob_wide_grad_kernel(const __grid_con
       }
       if (i >= i1) continue;
       float v[N], o[N];
+      if (MASK) Vec<T>::template hide<Vec<T>::NEG_INF_BITS>(r, on[k]);
       Vec<T>::unpack(r, v);
       const int j0 = head + i * N;
-      if (MASK) {
 #pragma unroll
-        for (int j = 0; j < N; ++j)
-          if (!(on[k][j / 4] >> (8 * (j & 3)) & 0xFF)) v[j] = -INFINITY;
+      for (int j = 0; j < N; j += 2) {
+        const float2 t = entry_grad2(m2, c2, ls2, k2, h2, v[j], v[j + 1]);
+        o[j] = t.x;
+        o[j + 1] = t.y;
       }
-#pragma unroll
-      for (int j = 0; j < N; ++j) o[j] = entry_grad(g.m, g.ls2, g.k, g.h, v[j], c);
       if ((unsigned)(g.action - j0) < (unsigned)N) {
 #pragma unroll
         for (int j = 0; j < N; ++j)
