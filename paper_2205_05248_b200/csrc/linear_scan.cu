@@ -198,22 +198,39 @@ struct ScanShared {
   uint8_t cut[2][MAX_WARPS];
 };
 
-// The state that enters chunk `chunk` of the time axis from the maps of the chunks before it (backward: behind it).
+// The state that enters a chunk of the time axis (BACK: the gradient that comes back into it) behind `count` others.  A block has one unit
+// then: its warps compose an eighth of the chunks' maps each.
 template <int V, bool BACK>
-__device__ __forceinline__ void enter_chunk(const ScanParams& p, const Place& w, int chunk, int used, float (&h)[V]) {
+__device__ __forceinline__ void enter_chunk(const ScanParams& p, const Place& w, ScanShared& sh, int count, int used, float (&h)[V]) {
   const float2* agg = p.agg + (long long)w.b * p.chunks * p.C + w.c;
   const uint8_t* cut = p.agg_cut + ((long long)w.b * p.groups + w.group) * p.chunks;
-  const int n = BACK ? used - 1 - chunk : chunk;
+  const int per = (count + MAX_WARPS - 1) / MAX_WARPS, i0 = w.warp * per, i1 = min(count, i0 + per), ch = w.lane & ((1 << p.lg) - 1);
+  Map m[V];
+#pragma unroll
+  for (int v = 0; v < V; ++v) m[v] = Map{1.f, 0.f, false};
 #pragma unroll 8
-  for (int i = 0; i < n; ++i) {
+  for (int i = i0; i < i1; ++i) {
     const int at = BACK ? used - 1 - i : i;
     const bool c = cut[at];
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-      const float2 m = w.on ? agg[(long long)at * p.C + v] : make_float2(0.f, 0.f);
-      h[v] = apply(Map{m.x, m.y, c}, h[v]);
+      const float2 t = w.on ? agg[(long long)at * p.C + v] : make_float2(0.f, 0.f);
+      m[v] = then(m[v], Map{t.x, t.y, c});
     }
   }
+  if (w.sub == 0) {
+#pragma unroll
+    for (int v = 0; v < V; ++v) sh.total[0][w.warp][ch * V + v] = make_float2(m[v].a, m[v].h);
+    if (ch == 0) sh.cut[0][w.warp] = m[0].cut;
+  }
+  __syncthreads();
+  for (int i = 0; i < MAX_WARPS; ++i)
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      const float2 t = sh.total[0][i][ch * V + v];
+      h[v] = apply(Map{t.x, t.y, (bool)sh.cut[0][i]}, h[v]);
+    }
+  __syncthreads();
 }
 
 // AGG: only the chunk's map is computed, for the launch behind this one.
@@ -232,7 +249,7 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 4) scan_kernel(const __grid_co
     carry[v] = !AGG && w.on && p.h0 ? p.h0[(long long)w.b * p.C + w.c + v] : 0.f;
     whole[v] = Map{1.f, 0.f, false};
   }
-  if (!AGG && p.chunks > 1 && first < w.n) enter_chunk<V, false>(p, w, blockIdx.y, 0, carry);
+  if (!AGG && p.chunks > 1 && first < w.n) enter_chunk<V, false>(p, w, sh_all, blockIdx.y, 0, carry);
   int par = 0;
   for (int k0 = first; k0 < end; k0 += tile, par ^= 1) {
     const int mine = k0 + w.q * S;
@@ -357,7 +374,7 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 2) scan_grad_kernel(const __gr
     carry[v] = !AGG && w.on && p.dlast && !gone ? p.dlast[(long long)w.b * p.C + w.c + v] : 0.f;
     whole[v] = Map{1.f, 0.f, false};
   }
-  if (!AGG && p.chunks > 1 && first < w.n) enter_chunk<V, true>(p, w, blockIdx.y, used, carry);
+  if (!AGG && p.chunks > 1 && first < w.n) enter_chunk<V, true>(p, w, sh_all, used - 1 - (int)blockIdx.y, used, carry);
   T* dg = reinterpret_cast<T*>(p.dg) + (long long)w.b * p.L * p.C + w.c;
   T* dx = reinterpret_cast<T*>(p.dx) + (long long)w.b * p.L * p.C + w.c;
   const int tiles = first < end ? (end - first + tile - 1) / tile : 0;
