@@ -421,7 +421,8 @@ int marl_policy_logprob(void* stream, const marl_policy_rows_t* in, int32_t top,
  * for available entries, 0 for the others, for empty rows, and (its first term) for rows without an action.  g_logp and
  * g_entropy f32[rows], either may be NULL (no gradient from there).  dlogits [rows][n_actions] of in->dtype, rows dlogits_stride (>= n_actions) elements
  * apart, is written in full; what lies between its rows is left as it is.  It may be the logits themselves (same address and row
- * distance).  The alternatives have no gradient. */
+ * distance).  The alternatives have no gradient.  A g that is not finite makes the gradient of its row's entries NaN, unavailable ones among
+ * them (not that of an empty row). */
 int marl_policy_logprob_backward(void* stream, const marl_policy_rows_t* in, const float* stats, const float* entropy,
                                  const float* g_logp, const float* g_entropy, void* dlogits, int64_t dlogits_stride);
 
@@ -478,7 +479,7 @@ int marl_linear_scan_backward(void* stream, const marl_scan_t* in, const float* 
 #define MARL_ORTHO_MAX_LONG 1024
 typedef struct {
   const void* in;               /* matrix k: element (r, c) at in[k * in_batch + r * in_row + c], strides >= 0 in elements */
-  void* out;                    /* likewise; may be the input itself (same address and strides) */
+  void* out;                    /* likewise; may be the entry's own input (same address and strides), must not overlap anything else of the list */
   int64_t in_batch, in_row, out_batch, out_row;
   int32_t batch, rows, cols;    /* batch >= 0; rows, cols >= 1 */
   float scale;

@@ -375,6 +375,8 @@ extern "C" int marl_orthogonalise(void* stream, const marl_matrix_t* list, int32
       return fail(MARL_EINVAL, "matrix %d: rows or matrices of the output overlap", i);
     if (misaligned(g.in, dtype_bytes(dtype)) || misaligned(g.out, dtype_bytes(dtype)))
       return fail(MARL_EALIGN, "matrix %d is not aligned to its elements", i);
+    for (int j = 0; j < i; ++j)
+      if (list[j].batch > 0 && list[j].out == g.out) return fail(MARL_EINVAL, "matrices %d and %d have the same output", j, i);
   }
   for (int i0 = 0; i0 < count;) {
     OrthoParams p = {};

@@ -322,3 +322,20 @@ def test_refusals():
     for a in ((r["states"][:, :0], dy), (r["states"], dy.half()), (r["states"], dy[:, :4])):
         with pytest.raises(e):
             g(gate, x, *a, **kw)
+
+
+def test_gradient_arrays_on_other_boundaries_than_the_inputs():
+    """The states that the forward pass kept serve every form of the gradient: dy that starts off a 16-byte boundary, and strided dy."""
+    for dt, B, L, C in (("fp32", 3, 150, 64), ("bf16", 2, 200, 72)):
+        gate, x, kw, dy, dlast = _make(B, L, C, dt, "blend", 3)
+        r = binding.marl_linear_scan(gate, x, keep=True, **kw)
+        want = binding.marl_linear_scan_backward(gate, x, r["states"], dy, dlast=dlast, **kw)
+        for off, pad in ((1, 0), (8, 3), (0, 8)):
+            buf = torch.empty(B * L * (C + pad) + 16, dtype=DT[dt], device="cuda")
+            v = buf[off:off + B * L * (C + pad)].view(B, L, C + pad)[..., :C]
+            v.copy_(dy)
+            got = binding.marl_linear_scan_backward(gate, x, r["states"], v, dlast=dlast, **kw)
+            w = _want(gate, x, kw, "blend", False, dy, dlast)
+            for k in ("dgate", "dx", "dh0"):
+                _close(got[k], w[k], k)
+                assert float((got[k].float() - want[k].float()).abs().max()) < 0.1

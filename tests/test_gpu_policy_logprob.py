@@ -5,7 +5,7 @@ constant), ex2.approx is within 2^-22, and a lane adds up to A/32 terms one afte
 error of S is below 2^-23 (A/64 + 2 U + 16), which is the absolute error of log S; (x_a - m) / T adds 2 U 2^-24 and each stored number half a step.
 Entropy is log S - V / S: V's terms carry another factor u <= U, so (1 + U) times that.  A gradient p (g + h (log p + H)) has p's
 relative error and h p times the errors of log p and H, then the rounding to its type, half a step relative (and half the
-smallest subnormal of fp16, 2^-25)."""
+smallest subnormal of fp16, 2^-25).  Probabilities below 2^-126 are flushed to 0."""
 import math
 
 import pytest
@@ -94,6 +94,8 @@ def _check(x, av, act, T=1.0, top=0, grads=True, gl=None, ge=None, out=None):
     rel = (2 * e + 4 * w["U"] * half + 2.0 ** -21)[:, None]
     mag = (gd.abs() * (hot + w["p"]) + hd.abs() * w["p"] * (lp0.abs() + w["H"][:, None] + 2 + w["U"][:, None])) / T
     tol = rel * mag + torch.finfo(x.dtype).eps / 2 * want.abs() + (2.0 ** -25 if x.dtype == torch.float16 else 1e-44)
+    # ex2 flushes: a probability below 2^-126 counts as 0, which takes up to 2^-126 (|g| + |h| |log p + H|) / T from its gradient
+    tol = tol + 2.0 ** -126 * (gd.abs() + hd.abs() * (lp0.abs() + w["H"][:, None])) / T
     _close(d, want, tol, "dlogits")
     assert bool((d[~w["on"]] == 0).all())
     return r, w
@@ -308,3 +310,38 @@ def test_large_values_in_few_lanes(R, A):
         act = torch.zeros(R, dtype=torch.int32, device="cuda")
         for top in (1, 5, 32):
             _check(x, None, act, top=top, grads=False)
+
+
+@pytest.mark.parametrize("dt", ["fp32", "bf16", "fp16"])
+@pytest.mark.parametrize("A", [13, 600, 9000])
+def test_temperatures_from_greedy_to_uniform(A, dt):
+    """Temperatures at which one value takes all, and at which the largest and the lowest number of the type are alike."""
+    x, av, act = _make(6, A, dt, A, True)
+    for T in (1e-4, 0.05, 40.0, 3e3, 1e6, 1e30):
+        _check(x, av, act, T=T, top=4)
+    x[1] = torch.finfo(x.dtype).min
+    x[2, ::3] = torch.finfo(x.dtype).min
+    av[1:3] = 1
+    for T in (0.5, 1e6, 1e30):
+        r = binding.marl_policy_logprob(x, act, avail=av, temperature=T, top=min(A, 32))
+        w = _want(x, av, act, T, min(A, 32))
+        assert torch.equal(r["top_index"].long(), w["ti"])
+        for k, v in (("logp", w["logp"]), ("entropy", w["H"])):
+            # (a log probability below fp32's lowest number is -infinity there; otherwise it has that many of its own steps, and
+            # log S and the entropy their errors as above, U being below 150 where a term counts)
+            f = torch.isfinite(v.float())
+            lim = 1e-3 * (1 + math.log(A)) + 2.0 ** -20 * v.abs()
+            assert torch.equal(torch.isfinite(r[k]), f) and bool(((r[k].double() - v).abs() < lim)[f].all()), (T, k)
+
+
+def test_a_gradient_that_is_not_finite_stays_in_its_row():
+    for A in (14, 500):
+        x, av, act = _make(6, A, "fp32", 0, True)
+        act[:] = 0
+        r = binding.marl_policy_logprob(x, act, avail=av)
+        g = torch.ones(6, device="cuda")
+        clean = binding.marl_policy_logprob_backward(x, act, r["stats"], r["entropy"], g_logp=g, avail=av)
+        g[2], g[3] = math.nan, math.inf                      # row 3 is empty
+        d = binding.marl_policy_logprob_backward(x, act, r["stats"], r["entropy"], g_logp=g, avail=av)
+        keep = torch.tensor([0, 1, 3, 4, 5], device="cuda")
+        assert torch.equal(d[keep], clean[keep]) and bool((d[3] == 0).all()) and bool(torch.isnan(d[2]).any())

@@ -178,6 +178,12 @@ def test_orthogonalise_arguments_are_refused(lib):
     assert _ortho(lib, []) == 0 and _ortho(lib, [_matrix(batch=0, in_=None, out=None)]) == 0
 
 
+def test_two_results_in_one_place_are_refused(lib):
+    a, b = _matrix(), _matrix(in_=GOOD + 4096)
+    assert _ortho(lib, [a, b]) == EINVAL and b"same output" in lib.marl_last_error()
+    assert _ortho(lib, [a, _matrix(out=GOOD + 8192), a]) == EINVAL
+
+
 def test_matrices_without_a_gpu_are_refused():
     with pytest.raises(binding.MarlError):
         binding.marl_orthogonalise([torch.zeros(4, 4)])
