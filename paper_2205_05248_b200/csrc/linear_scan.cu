@@ -1041,7 +1041,7 @@ static void plan(ScanParams& p, int V, bool pipe) {
   const long long blocks = ((long long)p.B * p.groups + p.units - 1) / p.units;
   p.chunks = 1;
   p.chunk_len = p.L > 0 ? p.L : 1;
-  if (blocks < 2 * SCAN_SMS && p.L >= 4 * tile) {
+  if (blocks > 0 && blocks < 2 * SCAN_SMS && p.L >= 4 * tile) {
     const int tiles = (p.L + tile - 1) / tile;
     int want = (int)((pipe ? 3 : 4) * SCAN_SMS / blocks);
     want = std::max(1, std::min(want, tiles / 2));

@@ -141,6 +141,14 @@ def test_scans_of_nothing(lib):
         assert lib.marl_linear_scan_backward(None, C.byref(s), None, None, 0, 0, None, None, None, None, None, 0) == 0
 
 
+def test_sizes_of_scans_of_nothing(lib):
+    """No sequences or channels, however long: no scratch (and no division by the number of blocks)."""
+    for over in (dict(B=0, L=100000), dict(C=0, L=100000), dict(B=0, C=0, L=1 << 20), dict(L=0)):
+        need, kept = C.c_size_t(7), C.c_size_t(7)
+        assert lib.marl_linear_scan_query(C.byref(_scan(**over)), C.byref(kept), C.byref(need)) == 0
+        assert need.value == 0 and kept.value == 0
+
+
 def test_scan_tensors_without_a_gpu_are_refused():
     x = torch.zeros(2, 3, 4)
     with pytest.raises(binding.MarlError):
