@@ -22,8 +22,9 @@ namespace cg = cooperative_groups;
 
 namespace marl {
 
-// 256 threads: 16 matrices of hidden 128 in 115 us, the 256 of 64 hidden-64 networks in 143; with 512 threads for the former 129 us, with 128 for
-// the latter 174 us.
+// 256 threads: 16 matrices of hidden 128 in 115 us, the 256 of 64 hidden-64 networks in 143 (133 with the products' loops unrolled by
+// eight in place of four); with 512 threads for the former 129 us, with 128 for the latter 174 us.  Loading the operands of the next k by hand while
+// those of this one are multiplied: 124 and 152 us.
 constexpr int ORTHO_GROUPS = 32, ORTHO_THREADS = 256;
 constexpr int ORTHO_SMS = 148;
 
@@ -94,7 +95,7 @@ __device__ __forceinline__ void square_tile(const float* s, int r0, int tx, int 
   for (int r = 0; r < R; ++r)
 #pragma unroll
     for (int j = 0; j < W; ++j) acc[r][j] = 0.f;
-#pragma unroll 4
+#pragma unroll 8
   for (int k = k0; k < k1; ++k) {
     float a[R], b[W];
     load_rows<R>(s + k * MP + r0, a);
@@ -187,7 +188,7 @@ __device__ void ortho_matrix(const OrthoParams& p, const OrthoGroup& g, int inde
 #pragma unroll
         for (int j = 0; j < W; ++j) acc[i][j] = 0.f;
       if (ty < TY) {
-#pragma unroll 4
+#pragma unroll 8
         for (int k = 0; k < ns; ++k) {
           float a[H], b[W];
           load_rows<H>(xt + k * PITCH + ty * H, a);
