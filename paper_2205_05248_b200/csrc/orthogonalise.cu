@@ -9,7 +9,11 @@
 //   each block XT <- XT Q on its slice, in place (a row of XT depends on that row alone)
 // Everything between blocks is sent, nothing fetched: stores into another block's shared memory are not waited for, loads from it are.
 // The products are plain fp32 multiply-adds with register tiles: the polynomial's slope at 0 amplifies rounding errors of
-// small singular directions (c0^5 = 485), so operands of fewer bits would show in the result.
+// small singular directions (c0^5 = 485), so operands of fewer bits would show in the result: measured error 1.0e-6 (that of
+// the formula in torch's fp32 products: 1.4e-6), 17 times fp32's half step; as many of bf16's would be 3 %.
+// Measured, five steps: the four matrices of a hidden-64 network 39 us, 16 matrices of hidden 128 115 us (1.3 GFLOP: 11 TFLOP/s), 256 of hidden 64
+// 133 us (22 TFLOP/s).  Clocks of a step of 384 x 128 on eight blocks: shares of S 9 k (6.1 k if every clock multiplied), S S 4.4 k (2 k), X Q
+// 11.7 k (6.1 k), sending 8 k, barriers 6 k: two warps a scheduler do not cover the loads' latency, and more warps have too small tiles.
 #include "learner_util.cuh"
 #include "launch_util.cuh"
 
