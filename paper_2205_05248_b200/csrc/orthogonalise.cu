@@ -11,9 +11,9 @@
 // The products are plain fp32 multiply-adds with register tiles: the polynomial's slope at 0 amplifies rounding errors of
 // small singular directions (c0^5 = 485), so operands of fewer bits would show in the result: measured error 1.0e-6 (that of
 // the formula in torch's fp32 products: 1.4e-6), 17 times fp32's half step; as many of bf16's would be 3 %.
-// Measured, five steps: the four matrices of a hidden-64 network 39 us, 16 matrices of hidden 128 115 us (1.3 GFLOP: 11 TFLOP/s), 256 of hidden 64
-// 133 us (22 TFLOP/s).  Clocks of a step of 384 x 128 on eight blocks: shares of S 9 k (6.1 k if every clock multiplied), S S 4.4 k (2 k), X Q
-// 11.7 k (6.1 k), sending 8 k, barriers 6 k: two warps a scheduler do not cover the loads' latency, and more warps have too small tiles.
+// Measured, five steps: the four matrices of a hidden-64 network 37 us, 16 matrices of hidden 128 107 us (1.3 GFLOP: 12 TFLOP/s), 256 of hidden 64
+// 130 us (22 TFLOP/s).  Clocks of a step of 384 x 128 on eight blocks: shares of S 8.6 k (6.1 k if every clock multiplied), S S 3.7 k (2 k), X Q
+// 9 k (6.1 k), sending 10 k, barriers 5 k: the squares that every block needs whole cross the cluster three times at some 20 bytes a clock.
 #include "learner_util.cuh"
 #include "launch_util.cuh"
 
@@ -26,9 +26,8 @@ namespace cg = cooperative_groups;
 
 namespace marl {
 
-// 256 threads: 16 matrices of hidden 128 in 115 us, the 256 of 64 hidden-64 networks in 143 (133 with the products' loops unrolled by
-// eight in place of four); with 512 threads for the former 129 us, with 128 for the latter 174 us.  Loading the operands of the next k by hand while
-// those of this one are multiplied: 124 and 152 us.
+// 256 threads (with the products' lanes in a grid of 16 x 2: 16 matrices of hidden 128 in 115 us, with 512 threads 129; the 256 of 64 hidden-64
+// networks in 143, with 128 threads 174).
 constexpr int ORTHO_GROUPS = 32, ORTHO_THREADS = 256;
 constexpr int ORTHO_SMS = 148;
 
@@ -57,71 +56,65 @@ inline size_t ortho_smem(int m, int n, int cluster, int squares) {
 }
 constexpr size_t ORTHO_SMEM_MAX = 226 * 1024;
 
-// Columns of a 16-wide grid of threads: groups of four neighbours 64 apart where a thread has eight, so that a warp's 16-byte loads
-// meet every bank once.
-template <int W>
-__device__ __forceinline__ int col_of(int t, int i) { return W <= 4 ? t * W + i : (i >> 2) * 64 + t * 4 + (i & 3); }
-template <int W>
-__device__ __forceinline__ void load_cols(const float* row, int t, float (&v)[W]) {
-  if constexpr (W >= 4) {
+// N neighbouring floats, 16, 8 or 4 bytes a load.
+template <int N>
+__device__ __forceinline__ void load_floats(const float* at, float (&v)[N]) {
+  if constexpr (N % 4 == 0) {
 #pragma unroll
-    for (int i = 0; i < W; i += 4) *reinterpret_cast<float4*>(&v[i]) = *reinterpret_cast<const float4*>(row + col_of<W>(t, i));
-  } else {
-#pragma unroll
-    for (int i = 0; i < W; ++i) v[i] = row[t * W + i];
-  }
-}
-template <int W>
-__device__ __forceinline__ void store_cols(float* row, int t, const float (&v)[W]) {
-  if constexpr (W >= 4) {
-#pragma unroll
-    for (int i = 0; i < W; i += 4) *reinterpret_cast<float4*>(row + col_of<W>(t, i)) = *reinterpret_cast<const float4*>(&v[i]);
-  } else {
-#pragma unroll
-    for (int i = 0; i < W; ++i) row[t * W + i] = v[i];
-  }
-}
-
-// H neighbouring rows of a square, of one of its columns.
-template <int H>
-__device__ __forceinline__ void load_rows(const float* at, float (&v)[H]) {
-  if constexpr (H >= 4) {
-#pragma unroll
-    for (int i = 0; i < H; i += 4) *reinterpret_cast<float4*>(&v[i]) = *reinterpret_cast<const float4*>(at + i);
-  } else if constexpr (H == 2) *reinterpret_cast<float2*>(v) = *reinterpret_cast<const float2*>(at);
+    for (int i = 0; i < N; i += 4) *reinterpret_cast<float4*>(&v[i]) = *reinterpret_cast<const float4*>(at + i);
+  } else if constexpr (N == 2) *reinterpret_cast<float2*>(v) = *reinterpret_cast<const float2*>(at);
   else v[0] = at[0];
 }
+template <int N>
+__device__ __forceinline__ void store_floats(float* at, const float (&v)[N]) {
+  if constexpr (N == 4) *reinterpret_cast<float4*>(at) = *reinterpret_cast<const float4*>(v);
+  else if constexpr (N == 2) *reinterpret_cast<float2*>(at) = *reinterpret_cast<const float2*>(v);
+  else at[0] = v[0];
+}
 
-// A tile of R x W elements of S S: rows r0 .. r0 + R - 1, this thread's columns, over k0 <= k < k1.  (S is symmetric: its rows are read.)
-template <int MP, int R, int W>
-__device__ __forceinline__ void square_tile(const float* s, int r0, int tx, int k0, int k1, float (&acc)[R][W]) {
+// A warp's part of a product: acc[r][j] = sum over k0 <= k < k1 of rows[k][r] cols[k][j].  All lanes share the rows (one address: a broadcast) and
+// have W neighbouring columns each, so that H W multiply-adds a lane cost H / 4 broadcasts and one load of the whole row; rows go in
+// pairs through the packed multiply-add.  (Lanes in a grid of 16 x 2 with 8 x 8 elements each and single multiply-adds: 115 us for 16 matrices of
+// hidden 128 against 107.)
+template <int H, int W>
+__device__ __forceinline__ void outer_products(const float* rows, const float* cols, int pitch, int k0, int k1, float (&acc)[H][W]) {
+  float2 t[H / 2][W];
 #pragma unroll
-  for (int r = 0; r < R; ++r)
+  for (int r = 0; r < H / 2; ++r)
 #pragma unroll
-    for (int j = 0; j < W; ++j) acc[r][j] = 0.f;
+    for (int j = 0; j < W; ++j) t[r][j] = make_float2(0.f, 0.f);
 #pragma unroll 8
   for (int k = k0; k < k1; ++k) {
-    float a[R], b[W];
-    load_rows<R>(s + k * MP + r0, a);
-    load_cols<W>(s + k * MP, tx, b);
+    float a[H], b[W];
+    load_floats<H>(rows + k * pitch, a);
+    load_floats<W>(cols + k * pitch, b);
 #pragma unroll
-    for (int r = 0; r < R; ++r)
+    for (int j = 0; j < W; ++j) {
+      const float2 bb = make_float2(b[j], b[j]);
 #pragma unroll
-      for (int j = 0; j < W; ++j) acc[r][j] = fmaf(a[r], b[j], acc[r][j]);
+      for (int r = 0; r < H / 2; ++r) t[r][j] = fma2(make_float2(a[2 * r], a[2 * r + 1]), bb, t[r][j]);
+    }
   }
+#pragma unroll
+  for (int r = 0; r < H / 2; ++r)
+#pragma unroll
+    for (int j = 0; j < W; ++j) {
+      acc[2 * r][j] = t[r][j].x;
+      acc[2 * r + 1][j] = t[r][j].y;
+    }
 }
 
 template <typename T, int MP>
 __device__ void ortho_matrix(const OrthoParams& p, const OrthoGroup& g, int index, float* smem) {
-  constexpr int PITCH = pitch_of(MP), W = MP / 16;
-  // The threads form a grid of 16 columns (W columns of a square each) by ORTHO_THREADS / 16 rows, of which the first TY have H rows of a square each.
-  constexpr int ROWS = ORTHO_THREADS / 16, TY = ROWS < MP ? ROWS : MP, H = MP / TY;
+  // A warp has H rows of a square, a lane W of its columns (a square of 16: the upper lanes repeat the lower ones' work and store nothing).
+  constexpr int PITCH = pitch_of(MP), WARPS = ORTHO_THREADS / 32, H = MP / WARPS, W = MP < 32 ? 1 : MP / 32;
   cg::cluster_group cluster = cg::this_cluster();
   const int rank = (int)cluster.block_rank(), size = (int)cluster.num_blocks();
   const bool tall = g.rows > g.cols;
   const int m = tall ? g.cols : g.rows, n = tall ? g.rows : g.cols;
   const int ns = slice_of(n, size), j0 = rank * ns;
-  const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, col = (MP < 32 ? lane & (MP - 1) : lane) * W;
+  const bool stores = MP >= 32 || lane < MP;
   float* xt = smem;                       // [ns][PITCH]
   float* shares = xt + ns * PITCH;        // [size][MP / size][MP] the blocks' shares of this block's rows of S
   float* s = shares + MP * MP;            // [MP][MP]
@@ -187,27 +180,13 @@ __device__ void ortho_matrix(const OrthoParams& p, const OrthoGroup& g, int inde
   for (int step = 0; step < p.steps; ++step) {
     {  // this block's share of S
       float acc[H][W];
-#pragma unroll
-      for (int i = 0; i < H; ++i)
-#pragma unroll
-        for (int j = 0; j < W; ++j) acc[i][j] = 0.f;
-      if (ty < TY) {
-#pragma unroll 8
-        for (int k = 0; k < ns; ++k) {
-          float a[H], b[W];
-          load_rows<H>(xt + k * PITCH + ty * H, a);
-          load_cols<W>(xt + k * PITCH, tx, b);
-#pragma unroll
-          for (int i = 0; i < H; ++i)
-#pragma unroll
-            for (int j = 0; j < W; ++j) acc[i][j] = fmaf(a[i], b[j], acc[i][j]);
-        }
+      outer_products<H, W>(xt + warp * H, xt + col, PITCH, 0, ns, acc);
+      if (stores)
 #pragma unroll
         for (int i = 0; i < H; ++i) {
-          const int row = ty * H + i, owner = row / rs;
-          store_cols<W>(cluster.map_shared_rank(shares, owner) + (rank * rs + row - owner * rs) * MP, tx, acc[i]);
+          const int row = warp * H + i, owner = row / rs;
+          store_floats<W>(cluster.map_shared_rank(shares, owner) + (rank * rs + row - owner * rs) * MP + col, acc[i]);
         }
-      }
     }
     cluster.sync();
     for (int i = tid; i < rs * MP / 4; i += ORTHO_THREADS) {
@@ -222,22 +201,16 @@ __device__ void ortho_matrix(const OrthoParams& p, const OrthoGroup& g, int inde
       for (int r = 0; r < size; ++r) reinterpret_cast<float4*>(cluster.map_shared_rank(s, r) + row0 * MP)[i] = t;
     }
     cluster.sync();
-    // This block's rows of S S, into `shares` (which is free now).  Tiles of R rows by MP / 16 columns keep the multiply-adds ahead of the
-    // loads; with few rows the threads that are left take parts of the sum over k, which are added up in their order.
-    int parts;
+    // This block's rows of S S, into `shares` (which is free now): its MP / size rows are `bands` tiles of H, and the warps that are left take parts
+    // of the sum over k, which are added up in their order.  (S is symmetric: its rows are read.)
+    const int bands = rs / H, parts = WARPS / bands, len = MP / parts;
     {
-      constexpr int R = H < 4 ? H : 4;
-      const int bands = rs / R;                     // of rows; 16 threads each
-      parts = bands >= TY ? 1 : TY / bands;         // (parts * rs <= MP rows of room)
-      const int len = MP / parts;
-      if (ty < TY && bands > 0)
-        for (int b = ty % bands; b < bands; b += TY) {  // (ty / bands: which part)
-          const int part = bands >= TY ? 0 : ty / bands;
-          float acc[R][W];
-          square_tile<MP, R, W>(s, row0 + b * R, tx, part * len, (part + 1) * len, acc);
+      const int band = warp % bands, part = warp / bands;
+      float acc[H][W];
+      outer_products<H, W>(s + row0 + band * H, s + col, MP, part * len, (part + 1) * len, acc);
+      if (stores)
 #pragma unroll
-          for (int r = 0; r < R; ++r) store_cols<W>(shares + (part * rs + b * R + r) * MP, tx, acc[r]);
-        }
+        for (int r = 0; r < H; ++r) store_floats<W>(shares + (part * rs + band * H + r) * MP + col, acc[r]);
     }
     __syncthreads();
     // this block's rows of Q, to every block
@@ -268,10 +241,10 @@ __device__ void ortho_matrix(const OrthoParams& p, const OrthoGroup& g, int inde
       for (int r = 0; r < size; ++r) reinterpret_cast<float4*>(cluster.map_shared_rank(qs, r) + row0 * MP)[tid + h * ORTHO_THREADS] = q[h];
     }
     cluster.sync();
-    // XT <- XT Q: the 16 threads of a row are lanes of one warp, so a row is read by them all before any of them writes it
+    // XT <- XT Q: a row belongs to one warp, whose lanes have all read it before any of them writes it
     auto times_q = [&](auto count) {
       constexpr int R = decltype(count)::value;
-      for (int b = ty * R; b < ns; b += ROWS * R) {
+      for (int b = warp * R; b < ns; b += WARPS * R) {
         float acc[R][W];
         const float* rows[R];
 #pragma unroll
@@ -288,24 +261,38 @@ __device__ void ortho_matrix(const OrthoParams& p, const OrthoGroup& g, int inde
 #pragma unroll
           for (int kk = 0; kk < 4; ++kk) {
             float q[W];
-            load_cols<W>(qs + (k + kk) * MP, tx, q);
+            load_floats<W>(qs + (k + kk) * MP + col, q);
 #pragma unroll
-            for (int i = 0; i < R; ++i)
+            for (int i = 0; i < R; ++i) {
+              if constexpr (W % 2 == 0) {
+                const float2 aa = make_float2(a[i][kk], a[i][kk]);
 #pragma unroll
-              for (int j = 0; j < W; ++j) acc[i][j] = fmaf(a[i][kk], q[j], acc[i][j]);
+                for (int j = 0; j < W; j += 2) {
+                  const float2 t = fma2(aa, make_float2(q[j], q[j + 1]), make_float2(acc[i][j], acc[i][j + 1]));
+                  acc[i][j] = t.x;
+                  acc[i][j + 1] = t.y;
+                }
+              } else {
+#pragma unroll
+                for (int j = 0; j < W; ++j) acc[i][j] = fmaf(a[i][kk], q[j], acc[i][j]);
+              }
+            }
           }
         }
-        __syncwarp(0xFFFFu << (tid & 16));
+        __syncwarp();
+        if (stores)
 #pragma unroll
-        for (int i = 0; i < R; ++i)
-          if (b + i < ns) store_cols<W>(xt + (b + i) * PITCH, tx, acc[i]);
-        __syncwarp(0xFFFFu << (tid & 16));
+          for (int i = 0; i < R; ++i)
+            if (b + i < ns) store_floats<W>(xt + (b + i) * PITCH + col, acc[i]);
+        __syncwarp();
       }
     };
-    if (ns > 3 * ROWS) times_q(std::integral_constant<int, 4>());
-    else if (ns > 2 * ROWS) times_q(std::integral_constant<int, 3>());
-    else if (ns > ROWS) times_q(std::integral_constant<int, 2>());
-    else times_q(std::integral_constant<int, 1>());
+    const int rows_a_warp = (ns + WARPS - 1) / WARPS;
+    if (rows_a_warp > 6) times_q(std::integral_constant<int, 8>());
+    else if (rows_a_warp > 4) times_q(std::integral_constant<int, 6>());
+    else if (rows_a_warp > 3) times_q(std::integral_constant<int, 4>());
+    else if (rows_a_warp > 2) times_q(std::integral_constant<int, 3>());
+    else times_q(std::integral_constant<int, 2>());
     if (p.squares == 3) __syncthreads();
     else cluster.sync();
   }
