@@ -435,9 +435,9 @@ int marl_policy_logprob_backward(void* stream, const marl_policy_rows_t* in, con
  * it is dropped if done[b][length[b] - 1] is set: the game had ended).  `last` is the state that passes on behind the last step: in
  * reverse y[b][0], forwards y[b][length[b] - 1], or 0 if done is set there; h0 for a sequence of length 0.  So a run over the
  * steps [0, s) and one over [s, L) with its `last` as h0 give what one run over [0, L) gives.
- * The state is held in fp32.  It is computed from products of neighbouring gates: raw gates are meant to be of modulus up to about 1,
- * and products of a few hundred of them that overflow fp32 give infinities or NaN; an infinite or NaN state stays on this side of a cut and
- * of its sequence and channel. */
+ * The state is held in fp32.  It is computed from products of neighbouring gates, up to all those between two cuts: raw gates are
+ * meant to be of modulus up to about 1, and where such a product overflows fp32 the states behind it may be infinite or NaN although the
+ * recurrence, step by step, would not be.  An infinite or NaN state stays on its side of a cut and in its sequence and channel. */
 #define MARL_SCAN_RAW 0
 #define MARL_SCAN_BLEND 1
 #define MARL_SCAN_INTERVAL 64 /* steps between two kept states */

@@ -345,3 +345,16 @@ def test_a_gradient_that_is_not_finite_stays_in_its_row():
         d = binding.marl_policy_logprob_backward(x, act, r["stats"], r["entropy"], g_logp=g, avail=av)
         keep = torch.tensor([0, 1, 3, 4, 5], device="cuda")
         assert torch.equal(d[keep], clean[keep]) and bool((d[3] == 0).all()) and bool(torch.isnan(d[2]).any())
+
+
+@pytest.mark.parametrize("A", [5, 14, 32, 40])
+def test_neighbouring_numbers_are_ranked_exactly(A):
+    """Values one step of fp32 apart, in ascending and in mixed order, around powers of two, zero and below it."""
+    for base in (1.0, -1.0, 2.0 ** -20, 1024.0):
+        b = torch.tensor([base], dtype=torch.float32).view(torch.int32)
+        j = torch.arange(A, dtype=torch.int32)
+        rows = torch.stack([b + j, b - j, b + (j * 7) % A, b + j // 2, b + (A - j) // 3])
+        x = rows.view(torch.float32).cuda()
+        _check(x, None, torch.zeros(5, dtype=torch.int32, device="cuda"), top=min(A, 32), grads=False)
+    tiny = (torch.arange(A, dtype=torch.int32) * 3 % A).view(torch.float32)          # subnormal numbers and zero
+    _check(torch.stack([tiny, -tiny]).cuda(), None, torch.zeros(2, dtype=torch.int32, device="cuda"), top=min(A, 32), grads=False)
