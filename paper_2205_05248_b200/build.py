@@ -1,7 +1,7 @@
 """Builds the CUDA library in-tree: ``python -m paper_2205_05248_b200.build``.
 
-nvcc compiles every ``csrc/*.cu`` for sm_100a and links ``libmarl_actor.so`` next to this file.  The build
-is skipped when the library is newer than all sources.
+nvcc compiles every ``csrc/*.cu`` for sm_100a - side by side, a process per file - and links ``libmarl_actor.so`` next to this
+file.  The build is skipped when the library is newer than all sources.
 """
 from __future__ import annotations
 
@@ -9,6 +9,8 @@ import glob
 import os
 import subprocess
 import sys
+import tempfile
+from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
@@ -33,12 +35,19 @@ def build(force: bool = False, verbose: bool = False) -> str:
         return LIB
     nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
     tmp = LIB + f".{os.getpid()}.tmp"
-    cmd = [nvcc, *NVCC_FLAGS, "-shared", "-o", tmp, *sources()]
-    if verbose:
-        cmd.insert(1, "-Xptxas")
-        cmd.insert(2, "-v")
-        print(" ".join(cmd), flush=True)
-    subprocess.check_call(cmd)
+    extra = ["-Xptxas", "-v"] if verbose else []
+    with tempfile.TemporaryDirectory() as work:
+        def compile_one(src):
+            obj = os.path.join(work, os.path.basename(src) + ".o")
+            cmd = [nvcc, *extra, *NVCC_FLAGS, "-c", "-o", obj, src]
+            if verbose:
+                print(" ".join(cmd), flush=True)
+            subprocess.check_call(cmd)
+            return obj
+
+        with ThreadPoolExecutor(max_workers=len(os.sched_getaffinity(0))) as pool:
+            objects = list(pool.map(compile_one, sources()))
+        subprocess.check_call([nvcc, *NVCC_FLAGS, "-shared", "-o", tmp, *objects])
     os.replace(tmp, LIB)
     return LIB
 
