@@ -605,6 +605,7 @@ __global__ void scan_step_grad_kernel(const __grid_constant__ ScanParams p) {
 constexpr int PIPE_STEPS = 64, PIPE_CHANNELS = 64, PIPE_THREADS = 256, PIPE_WARPS = 8, PIPE_S = PIPE_STEPS / PIPE_WARPS;
 constexpr int PIPE_BLOCKS = 4;
 template <typename T> constexpr int PIPE_SLOTS = sizeof(T) == 4 ? 2 : 3;
+constexpr int GRAD_SLOTS = 2;
 template <typename T, int ARRAYS> constexpr int SLOT_BYTES = ARRAYS * PIPE_STEPS * PIPE_CHANNELS * (int)sizeof(T);
 
 __device__ __forceinline__ float2 pair_of(const float* at) { return *reinterpret_cast<const float2*>(at); }
@@ -839,9 +840,10 @@ __global__ void __launch_bounds__(PIPE_THREADS, PIPE_BLOCKS) scan_pipe_kernel(co
   for (int t = max(n, first) + warp; t < stop; t += PIPE_WARPS) put_pair(y + (long long)t * p.C, make_float2(0.f, 0.f));
 }
 
-template <typename T, bool BLEND, bool CUT, bool AGG>
-__global__ void __launch_bounds__(PIPE_THREADS, 2) scan_pipe_grad_kernel(const __grid_constant__ ScanParams p) {
-  constexpr int SLOTS = PIPE_SLOTS<T>, ARRAYS = AGG ? 2 : 3, S = PIPE_S;
+// BLOCKS: blocks a multiprocessor, 2 (128 registers) or 3 (80).
+template <typename T, bool BLEND, bool CUT, bool AGG, int BLOCKS>
+__global__ void __launch_bounds__(PIPE_THREADS, BLOCKS) scan_pipe_grad_kernel(const __grid_constant__ ScanParams p) {
+  constexpr int SLOTS = GRAD_SLOTS, ARRAYS = AGG ? 2 : 3, S = PIPE_S;
   extern __shared__ __align__(16) uint8_t slots[];
   __shared__ PipeShared sh;
   const int lane = threadIdx.x & 31, warp = __shfl_sync(~0u, threadIdx.x >> 5, 0);
@@ -1154,7 +1156,7 @@ static int launch_scan(const ScanParams& p, bool grad, cudaStream_t stream) {
   return launch_ok("marl_linear_scan_backward");
 }
 
-static uint32_t g_pipe_smem[3][16][SMEM_OPTIN_DEVICES];
+static uint32_t g_pipe_smem[3][20][SMEM_OPTIN_DEVICES];
 
 template <typename T, bool BLEND, bool CUT>
 static int launch_pipe(const ScanParams& p, bool grad, int which, cudaStream_t stream) {
@@ -1170,14 +1172,20 @@ static int launch_pipe(const ScanParams& p, bool grad, int which, cudaStream_t s
     return cudaGetLastError();
   };
   cudaError_t e = cudaSuccess;
-  const int slots = std::min(PIPE_SLOTS<T>, (std::min(p.L, p.chunk_len) + PIPE_STEPS - 1) / PIPE_STEPS);  // no more than there are tiles
+  const int slots = std::min(grad ? GRAD_SLOTS : PIPE_SLOTS<T>, (std::min(p.L, p.chunk_len) + PIPE_STEPS - 1) / PIPE_STEPS);  // no more than there are tiles
   const int two = slots * SLOT_BYTES<T, 2>, three = slots * SLOT_BYTES<T, 3>;
   if (!grad) {
     if (p.chunks > 1) e = go(scan_pipe_kernel<T, BLEND, CUT, true>, two, w);
     if (e == cudaSuccess) e = go(scan_pipe_kernel<T, BLEND, CUT, false>, two, w + 4);
   } else {
-    if (p.chunks > 1) e = go(scan_pipe_grad_kernel<T, BLEND, CUT, true>, two, w + 8);
-    if (e == cudaSuccess) e = go(scan_pipe_grad_kernel<T, BLEND, CUT, false>, three, w + 12);
+    // Three blocks a multiprocessor where their shared memory allows it and they save a wave, else two, which are faster each: 64 x 256 x 512 bf16
+    // (two waves either way) 28 us with two and 33 with three, 8 x 4096 x 1024 bf16 (two waves and one) 187 and 159, 2048 x 64 x 256 fp32 (28
+    // and 19) 148 and 121.
+    const long long all = blocks * p.chunks;
+    auto waves = [&](long long per) { return (all + per * SCAN_SMS - 1) / (per * SCAN_SMS); };
+    const bool dense = 3 * three <= 200 * 1024 && waves(3) < waves(2);
+    if (p.chunks > 1) e = go(scan_pipe_grad_kernel<T, BLEND, CUT, true, 2>, two, w + 8);
+    if (e == cudaSuccess) e = dense ? go(scan_pipe_grad_kernel<T, BLEND, CUT, false, 3>, three, w + 16) : go(scan_pipe_grad_kernel<T, BLEND, CUT, false, 2>, three, w + 12);
   }
   return e == cudaSuccess ? MARL_OK : fail(MARL_ECUDA, "marl_linear_scan%s: %s", grad ? "_backward" : "", cudaGetErrorString(e));
 }
