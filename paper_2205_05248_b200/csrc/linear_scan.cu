@@ -12,9 +12,9 @@
 //
 // Forms: calls of one step (element by element), rows on 16-byte boundaries of 48 channels or more (tiles by asynchronous copies), and
 // everything else (direct loads, 1 to 32 lanes along the channels).  Measured (bytes bound all of them on paper):
-//   2048 x 64 x 256 fp32 blend: 68 us forward (5.9 TB/s), 148 us backward (4.5 TB/s)
-//   128 x 512 x 512 bf16 blend with cuts: 58 us forward (3.5 TB/s), 111 us backward (3.0 TB/s): 59 and 104 instructions for 64 elements; gates,
-//     conversions and the two barriers of a tile, with 27 and 16 warps a multiprocessor to cover them
+//   2048 x 64 x 256 fp32 blend: 68 us forward (5.9 TB/s), 121 us backward (5.5 TB/s)
+//   128 x 512 x 512 bf16 blend with cuts: 57 us forward (3.6 TB/s), 112 us backward (3.0 TB/s): 59 and 127 instructions for 64 elements; gates,
+//     conversions and the two barriers of a tile, with some 20 warps a multiprocessor to cover them
 //   65521 x 128 fp32 of one sequence: 37 us, two launches, the second reading from L2 what the first brought
 //   16384 x 512 bf16 of one step: 33 us, serving form of 24 x 64: 1.9 us
 #include "learner_util.cuh"
