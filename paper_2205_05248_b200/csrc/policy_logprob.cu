@@ -810,7 +810,9 @@ __global__ void __launch_bounds__(SMALL_ROWS) logprob_small_kernel(const __grid_
   const float ls = write_row(p, row, a, has, has ? mine[act] : -INFINITY);
   if (!p.top) return;
   // Keys that order like the values with their five lowest bits replaced by the index: one sort ranks them all, exactly where those bits
-  // are 0 (16-bit types) and nearly always in fp32; where two neighbours come out the wrong way round, and with NaN, one by one.
+  // are 0 (16-bit types) and nearly always in fp32.  There, numbers that differ in those bits only come out in the order of their indexes: the
+  // sorted places are looked through to the end of the group that the last wanted place lies in (a group of -infinities is in order), and where two
+  // neighbours are the wrong way round, or with NaN, the alternatives are taken one by one.
   int key[MA];
 #pragma unroll
   for (int j = 0; j < MA; ++j) {
@@ -819,15 +821,19 @@ __global__ void __launch_bounds__(SMALL_ROWS) logprob_small_kernel(const __grid_
   }
   sort_descending<0, MA>(key);
   bool exact = m == m;
-  float before = INFINITY;
+  if (sizeof(T) == 4) {
+    float before = INFINITY;
+    bool open = true;
 #pragma unroll
-  for (int k = 0; k < MA; ++k)
-    if (k <= p.top) {
+    for (int k = 0; k < MA; ++k) {
+      if (k > 0 && k >= p.top) open = open && (key[k] ^ key[k - 1]) >> 5 == 0 && before != -INFINITY;
+      if (!open) break;
       const int j = 31 - (key[k] & 31);
       const float x = j < A ? mine[j] : -INFINITY;
       exact = exact && x <= before;
       before = x;
     }
+  }
   int* ti = p.top_index + row * p.top;
   float* tl = p.top_logp + row * p.top;
   if (exact) {

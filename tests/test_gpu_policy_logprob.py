@@ -358,3 +358,48 @@ def test_neighbouring_numbers_are_ranked_exactly(A):
         _check(x, None, torch.zeros(5, dtype=torch.int32, device="cuda"), top=min(A, 32), grads=False)
     tiny = (torch.arange(A, dtype=torch.int32) * 3 % A).view(torch.float32)          # subnormal numbers and zero
     _check(torch.stack([tiny, -tiny]).cuda(), None, torch.zeros(2, dtype=torch.int32, device="cuda"), top=min(A, 32), grads=False)
+
+
+def _crowded_rows(A, seed):
+    """fp32 rows of numbers a few steps apart: whatever a ranking leaves out of their last bits, it has to look at them."""
+    g = torch.Generator().manual_seed(seed)
+    rows = []
+    for base in (1.0, -1.0, 2.0 ** -20, 1024.0):
+        b = torch.tensor([base], dtype=torch.float32).view(torch.int32)
+        for span in (2, 4, 12, 33, 41):                               # steps between the least and the largest, equal ones among them
+            j = torch.randint(0, span, (20, A), generator=g, dtype=torch.int32)
+            rows.append((b + j).view(torch.float32))
+        up = torch.tensor([0, 0, 1, 2, 1, 3, 40, 1], dtype=torch.int32)   # the largest last, behind a prefix that does not ascend
+        for k in range(4):
+            rows.append((b + up.roll(k).repeat(5)[:A][None]).view(torch.float32))
+    rows.append(20.0 + 1e-4 * torch.randn(100, A, generator=g))       # heads that are nearly equal
+    rows.append(10000.0 + 0.01 * torch.randn(100, A, generator=g))
+    half = 2.0 * torch.randn(100, A, generator=g)                     # half of a row close together, the rest apart
+    near = half.max() + 1.0 + 2.0 ** -20 * torch.randint(0, 16, (100, A), generator=g)
+    rows.append(torch.where(torch.rand(100, A, generator=g) < 0.5, near, half))
+    return torch.cat(rows)
+
+
+@pytest.mark.parametrize("A", [2, 3, 5, 8, 9, 14, 16, 17, 31, 32, 33])
+def test_fewer_alternatives_than_close_values_are_ranked_exactly(A):
+    """The best few of rows in which more values than those lie close together, with and without a mask."""
+    x = _crowded_rows(A, A)
+    R = x.shape[0]
+    av = (torch.rand(R, A, generator=torch.Generator().manual_seed(1)) < 0.8).to(torch.uint8)
+    act = torch.zeros(R, dtype=torch.int32).cuda()
+    buf = torch.zeros(R, A + 3)
+    buf[:, :A] = x
+    for top in sorted({1, 2, 3, 4, A // 2, A - 2, A - 1} - {0, -1}):
+        for rows in (x.cuda(), buf.cuda()[:, :A]):                    # without gaps, and rows of a wider buffer
+            for mask in (None, av.cuda()):
+                _check(rows, mask, act, top=top, grads=False)
+
+
+@pytest.mark.parametrize("dt", ["bf16", "fp16"])
+def test_close_values_of_16_bit_types_are_ranked_exactly(dt):
+    for A in (3, 14, 32):
+        g = torch.Generator().manual_seed(A)
+        one = torch.ones(1, dtype=DT[dt]).view(torch.int16)
+        x = (one + torch.randint(-3, 4, (200, A), generator=g, dtype=torch.int16)).view(DT[dt]).cuda()
+        for top in (1, 2, A - 1):
+            _check(x, None, torch.zeros(200, dtype=torch.int32, device="cuda"), top=top, grads=False)
