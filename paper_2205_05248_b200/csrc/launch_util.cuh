@@ -2,6 +2,7 @@
 #pragma once
 #include <cuda_runtime.h>
 #include <cstdint>
+#include <mutex>
 
 namespace marl {
 
@@ -9,15 +10,26 @@ constexpr int SMEM_OPTIN_DEVICES = 64;
 
 // A kernel's opt-in dynamic shared-memory size is a per-device setting.  `table` (one per kernel variant, zero
 // initialised) remembers the largest size set on each device, so that the attribute call is made once per device
-// and size instead of once per launch; devices beyond the table are set on every launch.
+// and size instead of once per launch; on devices beyond the table the runtime is asked for it.  Host threads may come
+// here at once with different sizes: the setting is changed by one of them at a time, only ever raised, and noted after it is made.
 inline cudaError_t ensure_dynamic_smem(const void* kernel, uint32_t bytes, uint32_t (&table)[SMEM_OPTIN_DEVICES]) {
+  static std::mutex raising;
   int dev = -1;
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return e;
   const bool tracked = dev >= 0 && dev < SMEM_OPTIN_DEVICES;
-  if (tracked && table[dev] >= bytes) return cudaSuccess;
+  if (tracked && __atomic_load_n(&table[dev], __ATOMIC_ACQUIRE) >= bytes) return cudaSuccess;
+  std::lock_guard<std::mutex> lock(raising);
+  if (tracked) {
+    if (table[dev] >= bytes) return cudaSuccess;
+  } else {
+    cudaFuncAttributes now;
+    e = cudaFuncGetAttributes(&now, kernel);
+    if (e != cudaSuccess) return e;
+    if (now.maxDynamicSharedSizeBytes >= (int)bytes) return cudaSuccess;
+  }
   e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
-  if (e == cudaSuccess && tracked) table[dev] = bytes;
+  if (e == cudaSuccess && tracked) __atomic_store_n(&table[dev], bytes, __ATOMIC_RELEASE);
   return e;
 }
 
