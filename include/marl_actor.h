@@ -481,11 +481,12 @@ typedef struct {
   const void* in;               /* matrix k: element (r, c) at in[k * in_batch + r * in_row + c], strides >= 0 in elements */
   void* out;                    /* likewise; may be the entry's own input (same address and strides), must not overlap anything else of the list */
   int64_t in_batch, in_row, out_batch, out_row;
-  int32_t batch, rows, cols;    /* batch >= 0; rows, cols >= 1 */
+  int32_t batch, rows, cols;    /* batch 0 .. 2^24; rows, cols >= 1 */
   float scale;
 } marl_matrix_t;
 
-/* list: HOST array of `count` entries, read before the call returns.  dtype: of all matrices.  steps 0 .. 64; eps >= 0. */
+/* list: HOST array of `count` entries, read before the call returns; all are checked before any is worked on.  dtype: of all matrices.
+ * steps 0 .. 64; eps >= 0. */
 int marl_orthogonalise(void* stream, const marl_matrix_t* list, int32_t count, int32_t dtype, int32_t steps, const float* coeffs, float eps);
 
 /* Name of the step kernel in use: "ffma" (the general path: split-operand tensor-core or CUDA-core kernel), "tcgen05"

@@ -30,6 +30,7 @@ namespace marl {
 // networks in 143, with 128 threads 174).
 constexpr int ORTHO_GROUPS = 32, ORTHO_THREADS = 256;
 constexpr int ORTHO_SMS = 148;
+constexpr int ORTHO_MAX_BATCH = 1 << 24;  // matrices an entry, and a launch
 
 struct OrthoGroup {
   const void* in;
@@ -360,6 +361,7 @@ extern "C" int marl_orthogonalise(void* stream, const marl_matrix_t* list, int32
     if (g.rows < 1 || g.cols < 1 || std::min(g.rows, g.cols) > MARL_ORTHO_MAX_SHORT || std::max(g.rows, g.cols) > MARL_ORTHO_MAX_LONG)
       return fail(MARL_EINVAL, "matrix %d: %d x %d is outside 1 x 1 .. %d x %d (either way round)", i, g.rows, g.cols, MARL_ORTHO_MAX_SHORT,
                   MARL_ORTHO_MAX_LONG);
+    if (g.batch > ORTHO_MAX_BATCH) return fail(MARL_EINVAL, "matrix %d: batch is larger than 2^24", i);
     if (g.batch == 0) continue;
     if (!g.in || !g.out) return fail(MARL_EINVAL, "matrix %d: in or out is NULL", i);
     if (g.in_batch < 0 || g.in_row < 0) return fail(MARL_EINVAL, "matrix %d: a stride is negative", i);
@@ -382,10 +384,7 @@ extern "C" int marl_orthogonalise(void* stream, const marl_matrix_t* list, int32
     for (; i < count && p.groups < ORTHO_GROUPS; ++i) {
       const marl_matrix_t& g = list[i];
       if (g.batch == 0) continue;
-      if (matrices + g.batch > (1 << 24)) {
-        if (p.groups == 0) return fail(MARL_EINVAL, "matrix %d: batch is larger than 2^24", i);
-        break;
-      }
+      if (matrices + g.batch > ORTHO_MAX_BATCH) break;  // (no single entry is larger: the first of a launch always fits)
       p.g[p.groups++] = OrthoGroup{g.in, g.out, g.in_batch, g.in_row, g.out_batch, g.out_row, (int)matrices, g.rows, g.cols, g.scale};
       matrices += g.batch;
     }

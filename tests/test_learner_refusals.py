@@ -196,3 +196,11 @@ def test_matrices_without_a_gpu_are_refused():
     with pytest.raises(binding.MarlError):
         binding.marl_orthogonalise([torch.zeros(4, 4)])
     assert binding.marl_orthogonalise([]) == []
+
+
+def test_a_list_with_an_entry_too_many_is_refused_whole(lib):
+    """The refusal of a later entry comes before any work on the ones in front of it, however the list is cut into launches."""
+    big = dict(out=GOOD + 65536, batch=(1 << 24) + 1)
+    assert _ortho(lib, [_matrix(**big)]) == EINVAL
+    assert _ortho(lib, [_matrix(), _matrix(**big)]) == EINVAL and b"2^24" in lib.marl_last_error()
+    assert _ortho(lib, [_matrix(out=GOOD + (1 << 16) * k) for k in range(40)] + [_matrix(**dict(big, out=GOOD + (1 << 30)))]) == EINVAL
