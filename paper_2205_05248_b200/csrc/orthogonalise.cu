@@ -18,6 +18,7 @@
 #include "launch_util.cuh"
 
 #include <algorithm>
+#include <cfloat>
 #include <cmath>
 #include <cooperative_groups.h>
 #include <type_traits>
@@ -168,7 +169,13 @@ __device__ void ortho_matrix(const OrthoParams& p, const OrthoGroup& g, int inde
   cluster.sync();
   sum = 0.f;
   for (int r = 0; r < size; ++r) sum += *cluster.map_shared_rank(&exchange[1], r);
-  const float norm = top * sqrtf(sum) + p.eps;
+  float norm = top * sqrtf(sum) + p.eps;
+  if (top > 0.f && !(norm >= FLT_MIN && norm <= FLT_MAX)) {
+    // beyond fp32's numbers, or below its normal ones, although no entry is: entries and eps relative to the largest entry
+#pragma unroll 1
+    for (int i = tid; i < live * MP; i += ORTHO_THREADS) xt[i / MP * PITCH + i % MP] /= top;
+    norm = sqrtf(sum) + p.eps / top;
+  }
   for (int i = tid; i < live * MP; i += ORTHO_THREADS) {
     const int j = i / MP, c = i - j * MP;
     float& v = xt[j * PITCH + c];

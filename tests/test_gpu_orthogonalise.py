@@ -153,3 +153,36 @@ def test_refusals():
                dict(out=[a.half()]), dict(out=[a[:, :1].expand(8, 9)])):
         with pytest.raises(e):
             f([a], **kw)
+
+
+@pytest.mark.parametrize("dt", ["fp32", "bf16"])
+@pytest.mark.parametrize("r,c", [(1, 2), (20, 33), (64, 102), (128, 1024)])
+@pytest.mark.parametrize("top", [3e38, 1e38, 2e36])
+def test_norms_beyond_fp32(r, c, top, dt):
+    """Finite matrices whose norm is not a number of fp32, beside one whose norm is.  Their scale is taken out in 64 bits for the fp32 evaluation that
+    the tolerance counts from; eps is as large as the entries once."""
+    base = _rand(r, c, seed=r)
+    m = (base / base.abs().max() * top).to(DT[dt])
+    assert bool(torch.isfinite(m).all())
+    for eps in (0.0, 1e-7, 1e38):
+        got = binding.marl_orthogonalise([m, base.to(DT[dt])], eps=eps)[0]
+        small = (m.double() * 2.0 ** -120).float()                       # exact
+        want = _formula(m.double(), eps=eps)
+        off32 = (_formula(small, eps=eps * 2.0 ** -120).double() - want).norm()
+        err, n = (got.double() - want).norm(), want.norm()
+        assert float(n) > 0.1
+        # (the quotients of the scaled norm and eps round twice more: 2^-23, and the polynomial passes a relative change of scale on by at most
+        # its largest slope a step where singular values are small: 3.4445^5 = 485 of those)
+        assert float(err) <= float(3 * off32 + (torch.finfo(got.dtype).eps / 2 + 2.0 ** -22 + 485 * 2.0 ** -23) * n), (eps, float(err / n))
+
+
+def test_norms_below_the_normal_numbers():
+    """Without eps the scale does not matter, however few bits the norm would have as a number of fp32."""
+    for r, c in ((1, 2), (20, 33), (100, 64)):
+        m = _rand(r, c, seed=c) * 1e-43
+        assert float(m.abs().max()) > 0
+        got = binding.marl_orthogonalise([m], eps=0.0)[0]
+        want = _formula(m.double(), eps=0.0)
+        off32 = (_formula((m.double() * 2.0 ** 120).float(), eps=0.0).double() - want).norm()
+        err, n = (got.double() - want).norm(), want.norm()
+        assert float(err) <= float(3 * off32 + (2.0 ** -22 + 485 * 2.0 ** -23) * n), (r, c, float(err / n))
