@@ -6,8 +6,9 @@
 //
 // Three forms of the pass: a thread per row up to 32 actions, a warp per row up to 4096, a block per row beyond, or the blocks of a cluster
 // where there are few rows.  Bytes bound all of them on paper; what bounds them measured:
-//   1024 x 96 x 8 rows of 14, fp32, availability: 13.5 us without alternatives (5.2 TB/s), 26 us with four - the ranking's integer
-//     minima and maxima run at half rate - and 20.6 us for the gradient (5.7 TB/s, part of it from L2)
+//   1024 x 96 x 8 rows of 14, fp32, availability: 16.6 us without alternatives (4.3 TB/s), 27.5 us with four - the ranking's integer
+//     minima and maxima run at half rate - and 20.0 us for the gradient (5.9 TB/s); 52 us with four where most rows' values lie within 32 steps
+//     of fp32 of each other (20 + N(0, 1e-4)) and are ranked one by one
 //   2048 rows of 65537, bf16: 50 us without alternatives (5.4 TB/s), 71 us with eight - the rows' ends are chains of shuffles, barriers and
 //     reads, which the other blocks of the multiprocessor cover only in part - and 94 us for the gradient (5.7 TB/s)
 //   one row of 131072: 12 us on a cluster of eight blocks (49 us on one block)
@@ -745,8 +746,10 @@ __device__ __forceinline__ void sort_descending(int (&a)[N]) {
   }
 }
 
+// Blocks an SM: 36, 40 and 56 registers a thread, which the ranking needs.  Without the bound the look at close values makes it 48 and 76 in fp32:
+// 786432 x 14, none / four alternatives 18.4 / 28.0 us against 16.6 / 27.5, in spite of the bound's spills (4 bytes; 56 for up to 32 actions).
 template <typename T, int MA, bool DENSE>
-__global__ void __launch_bounds__(SMALL_ROWS) logprob_small_kernel(const __grid_constant__ RowsParams p, uint32_t inv_a) {
+__global__ void __launch_bounds__(SMALL_ROWS, MA == 8 ? 14 : MA == 16 ? 12 : 9) logprob_small_kernel(const __grid_constant__ RowsParams p, uint32_t inv_a) {
   __shared__ float xs[SMALL_ROWS * (MA + 1)];
   const long long row0 = (long long)blockIdx.x * SMALL_ROWS;
   const int rows = (int)(p.rows - row0 < SMALL_ROWS ? p.rows - row0 : SMALL_ROWS), A = p.A, pitch = A | 1, pad = pitch - A;
