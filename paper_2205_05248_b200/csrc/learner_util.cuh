@@ -10,6 +10,8 @@
 
 namespace marl {
 
+constexpr int LEARNER_SMS = 148;  // multiprocessors of a B200: what launches are laid out for
+
 int fail(int code, const char* fmt, ...);  // defined beside marl_last_error; returns code
 
 inline size_t dtype_bytes(int32_t dtype) { return dtype == MARL_DTYPE_FP32 ? 4 : 2; }

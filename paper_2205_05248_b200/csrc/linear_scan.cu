@@ -12,11 +12,16 @@
 //
 // Forms: calls of one step (element by element), rows on 16-byte boundaries of 48 channels or more (tiles by asynchronous copies), and
 // everything else (direct loads, 1 to 32 lanes along the channels).  Measured (bytes bound all of them on paper):
-//   2048 x 64 x 256 fp32 blend: 68 us forward (5.9 TB/s), 121 us backward (5.5 TB/s)
-//   128 x 512 x 512 bf16 blend with cuts: 57 us forward (3.6 TB/s), 112 us backward (3.0 TB/s): 59 and 127 instructions for 64 elements; gates,
+//   2048 x 64 x 256 fp32 blend: 67 us forward (6.0 TB/s), 115 us backward (5.8 TB/s)
+//   128 x 512 x 512 bf16 blend with cuts: 58 us forward (3.5 TB/s), 109 us backward (3.1 TB/s): 59 and 127 instructions for 64 elements; gates,
 //     conversions and the two barriers of a tile, with some 20 warps a multiprocessor to cover them
-//   65521 x 128 fp32 of one sequence: 37 us, two launches, the second reading from L2 what the first brought
-//   16384 x 512 bf16 of one step: 33 us, serving form of 24 x 64: 1.9 us
+//   65521 x 128 fp32 of one sequence: 40 us forward, 53 us backward: two launches each, the second reading from L2 what the first brought
+//   one step, forward / backward: 16384 x 512 bf16 29 / 36 us, serving form of 24 x 64 1.6 / 1.8 us; 1000000 x 1 67 / 74 us (a warp a sequence, with
+//     one lane of it at work)
+//   few channels, fp32, forward / backward: 1024 x 96 x 1 4.0 / 4.7 us, 512 x 2000 x 3 19 / 29 us, 1 x 1000000 x 1 18 / 22 us (a lane's steps come one
+//     number a load); a gate that is one number for all 128 x 512 x 64: 21 / 32 us, the same gate written out 24 / 30 us
+// Registers: the direct form's bounds (64 a thread forward, 128 backward) make it spill with two channels a lane, 56 to 88 bytes forward and up to 108
+// backward; the tiles' kernels spill 4 to 28 bytes.
 #include "learner_util.cuh"
 #include "launch_util.cuh"
 
@@ -27,7 +32,6 @@ namespace marl {
 
 constexpr int STEPS = 8;       // steps a thread holds
 constexpr int MAX_WARPS = 8;   // warps along time
-constexpr int SCAN_SMS = 148;
 
 struct ScanParams {
   const void *g, *x;
@@ -84,7 +88,9 @@ __device__ __forceinline__ void put(__nv_bfloat16* at, const float (&f)[2]) {
 __device__ __forceinline__ void put(__half* at, const float (&f)[2]) { *reinterpret_cast<__half2*>(at) = __floats2half2_rn(f[0], f[1]); }
 __device__ __forceinline__ void put(float* at, const float (&f)[2]) {}  // (fp32 has one channel a lane)
 
-// z = 1 / (1 + e^-g) and 1 - z = e^-g z, each accurate where it is small; below g = -87 z stays at 2^-126.
+// z = 1 / (1 + e^-g) and 1 - z = e^-g z, each relative to itself within (1.23 |g| + 8) 2^-24: the exponent g log2 e is rounded once, which
+// e^-g multiplies by |g| (1 - z at g = 20, 2e-9: 2e-6 of itself; a second term of the exponent would take three operations more a gate).  Where e^-g
+// is below 2^-126 it is 0, and below g = -87 z stays at 2^-126.
 __device__ __forceinline__ void gate_pair(float g, float& z, float& rest) {
   float t, r;
   asm("min.NaN.f32 %0, %1, 0f42FC0000;" : "=f"(t) : "f"(g * -1.4426950408889634f));  // at most 126
@@ -1053,9 +1059,9 @@ static void plan(ScanParams& p, int V, bool pipe) {
   const long long blocks = ((long long)p.B * p.groups + p.units - 1) / p.units;
   p.chunks = 1;
   p.chunk_len = p.L > 0 ? p.L : 1;
-  if (blocks > 0 && blocks < 2 * SCAN_SMS && p.L >= 4 * tile) {
+  if (blocks > 0 && blocks < 2 * LEARNER_SMS && p.L >= 4 * tile) {
     const int tiles = (p.L + tile - 1) / tile;
-    int want = (int)((pipe ? 3 : 4) * SCAN_SMS / blocks);
+    int want = (int)((pipe ? 3 : 4) * LEARNER_SMS / blocks);
     want = std::max(1, std::min(want, tiles / 2));
     const int per = (tiles + want - 1) / want;
     p.chunk_len = per * tile;
@@ -1182,7 +1188,7 @@ static int launch_pipe(const ScanParams& p, bool grad, int which, cudaStream_t s
     // (two waves either way) 28 us with two and 33 with three, 8 x 4096 x 1024 bf16 (two waves and one) 187 and 159, 2048 x 64 x 256 fp32 (28
     // and 19) 148 and 121.
     const long long all = blocks * p.chunks;
-    auto waves = [&](long long per) { return (all + per * SCAN_SMS - 1) / (per * SCAN_SMS); };
+    auto waves = [&](long long per) { return (all + per * LEARNER_SMS - 1) / (per * LEARNER_SMS); };
     const bool dense = 3 * three <= 200 * 1024 && waves(3) < waves(2);
     if (p.chunks > 1) e = go(scan_pipe_grad_kernel<T, BLEND, CUT, true, 2>, two, w + 8);
     if (e == cudaSuccess) e = dense ? go(scan_pipe_grad_kernel<T, BLEND, CUT, false, 3>, three, w + 16) : go(scan_pipe_grad_kernel<T, BLEND, CUT, false, 2>, three, w + 12);

@@ -30,7 +30,6 @@ namespace marl {
 // 256 threads (with the products' lanes in a grid of 16 x 2: 16 matrices of hidden 128 in 115 us, with 512 threads 129; the 256 of 64 hidden-64
 // networks in 143, with 128 threads 174).
 constexpr int ORTHO_GROUPS = 32, ORTHO_THREADS = 256;
-constexpr int ORTHO_SMS = 148;
 constexpr int ORTHO_MAX_BATCH = 1 << 24;  // matrices an entry, and a launch
 
 struct OrthoGroup {
@@ -408,7 +407,7 @@ extern "C" int marl_orthogonalise(void* stream, const marl_matrix_t* list, int32
     int cluster = 1;
     while (cluster < 8 && smem_for(cluster, 3) > ORTHO_SMEM_MAX) cluster *= 2;
     if (smem_for(cluster, 3) > ORTHO_SMEM_MAX) p.squares = 2;
-    while (cluster < 8 && matrices * cluster * 2 <= ORTHO_SMS) cluster *= 2;
+    while (cluster < 8 && matrices * cluster * 2 <= LEARNER_SMS) cluster *= 2;
     const size_t smem = smem_for(cluster, p.squares);
     int rc;
     int most = 0;

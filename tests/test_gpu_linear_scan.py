@@ -339,3 +339,35 @@ def test_gradient_arrays_on_other_boundaries_than_the_inputs():
             for k in ("dgate", "dx", "dh0"):
                 _close(got[k], w[k], k)
                 assert float((got[k].float() - want[k].float()).abs().max()) < 0.1
+
+
+@pytest.mark.parametrize("B,L,C", [(3, 1, 200), (2, 40, 3), (2, 64, 64), (1, 1000, 64)])
+def test_gates_far_from_zero(B, L, C):
+    """z = 1 / (1 + e^-g) and 1 - z where one of them is small, up to where e^-g leaves the normal numbers.
+
+    u = 2^-24.  g log2 e is rounded once and its constant is off by 0.23 u, so e^-g is off by 1.23 |g| u relative, and ex2.approx by 4 u.
+    With e = e^-g: d ln z = -e / (1 + e) d ln e and d ln (1 - z) = 1 / (1 + e) d ln e, to which the sum adds u and the quotient 2 u
+    (1 ulp), and 1 - z one product more.  So both are within (1.23 |g| + 8) u relative, and a result that multiplies them once more by
+    an input, or each other, within that sum and 2 u a product.  2^v below 2^-126 is flushed, and 1 - z is e z: both are off by up to 2^-126 there."""
+    n = B * L * C
+    g = torch.linspace(-100.0, 100.0, n).view(B, L, C)[:, torch.randperm(L, generator=torch.Generator().manual_seed(1))].contiguous().cuda()
+    x = (1.0 + torch.rand(B, L, C, generator=torch.Generator().manual_seed(2))).cuda()
+    cut = torch.ones(B, L, dtype=torch.uint8, device="cuda")                 # every step by itself: y = (1 - z) x
+    z, rest = torch.sigmoid(g.double()), torch.sigmoid(-g.double())
+    e = (1.23 * g.double().abs() + 8) * U
+
+    def close(got, want, rel, what):
+        err = (got.double() - want).abs()
+        tol = rel * want.abs() + 2.0 ** -125
+        assert bool((err <= tol).all()), (what, float((err / tol).max()))
+
+    for reverse in (False, True):
+        r = binding.marl_linear_scan(g, x, done=cut, form="blend", reverse=reverse, keep=True)
+        close(r["y"], rest * x.double(), e + 2 * U, "y")
+        dy = torch.ones_like(x)
+        d = binding.marl_linear_scan_backward(g, x, r["states"], dy, done=cut, form="blend", reverse=reverse)
+        close(d["dx"], rest, e + 2 * U, "dx")
+        close(d["dgate"], -x.double() * z * rest, 2 * e + 6 * U, "dgate")
+    if L == 1:
+        h0 = torch.ones(B, C, device="cuda")
+        close(binding.marl_linear_scan(g, torch.zeros_like(x), h0=h0, form="blend")["last"], z[:, 0], e[:, 0] + 2 * U, "z")
