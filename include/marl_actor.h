@@ -421,8 +421,8 @@ int marl_policy_logprob(void* stream, const marl_policy_rows_t* in, int32_t top,
  * for available entries, 0 for the others, for empty rows, and (its first term) for rows without an action.  g_logp and
  * g_entropy f32[rows], either may be NULL (no gradient from there).  dlogits [rows][n_actions] of in->dtype, rows dlogits_stride (>= n_actions) elements
  * apart, is written in full; what lies between its rows is left as it is.  It may be the logits themselves (same address and row
- * distance).  The alternatives have no gradient.  A g that is not finite makes the gradient of its row's entries NaN, unavailable ones among
- * them (not that of an empty row). */
+ * distance).  The alternatives have no gradient.  A g that is not finite, and a row whose results are NaN, make the gradient of the row's
+ * entries NaN, unavailable ones among them (not that of an empty row). */
 int marl_policy_logprob_backward(void* stream, const marl_policy_rows_t* in, const float* stats, const float* entropy,
                                  const float* g_logp, const float* g_entropy, void* dlogits, int64_t dlogits_stride);
 

@@ -403,3 +403,25 @@ def test_close_values_of_16_bit_types_are_ranked_exactly(dt):
         x = (one + torch.randint(-3, 4, (200, A), generator=g, dtype=torch.int16)).view(DT[dt]).cuda()
         for top in (1, 2, A - 1):
             _check(x, None, torch.zeros(200, dtype=torch.int32, device="cuda"), top=top, grads=False)
+
+
+@pytest.mark.parametrize("dt", ["fp32", "bf16"])
+@pytest.mark.parametrize("A", [14, 500, 9000])
+def test_the_gradient_of_a_row_that_is_not_a_number(A, dt):
+    """A NaN or +infinity among the available entries makes its own row NaN, all of it; an unavailable one has no effect."""
+    x, av, act = _make(8, A, dt, 3, True)
+    av[:, :3] = 1
+    av[4] = 0                                                     # an empty row
+    act[:] = 1
+    g = torch.ones(8, device="cuda")
+    kw = dict(g_logp=g, g_entropy=g, avail=av)
+    av[6, 2] = 0
+    r = binding.marl_policy_logprob(x, act, avail=av)
+    clean = binding.marl_policy_logprob_backward(x, act, r["stats"], r["entropy"], **kw)
+    x[1, 0], x[2, 2], x[6, 2], x[4, 5] = math.nan, math.inf, math.nan, math.nan
+    r = binding.marl_policy_logprob(x, act, avail=av)
+    d = binding.marl_policy_logprob_backward(x, act, r["stats"], r["entropy"], **kw)
+    bad = torch.zeros(8, dtype=torch.bool, device="cuda")
+    bad[1:3] = True
+    assert torch.equal(torch.isnan(r["logp"]), bad) and torch.equal(torch.isnan(r["entropy"]), bad)
+    assert bool(torch.isnan(d[1:3]).all()) and torch.equal(d[~bad], clean[~bad])
