@@ -216,14 +216,11 @@ def _dptr(t):
 
 
 # ---- the learner's operators (device tensors, on the current stream of their device) ------------------------------------
+# They are not part of autograd: results carry no graph, whether or not the inputs require gradients, and a gradient is asked for with
+# the *_backward function of the same name.  marl_orthogonalise has none.
 # Calls of a few microseconds of GPU work are common here, so the marshalling is kept short: no text is made unless a check
 # fails, the stream is asked for as a number, and dense outputs are made with their strides.
 _F32, _I32 = torch.float32, torch.int32
-
-
-def _need(ok: bool, text: str):
-    if not ok:
-        raise MarlError(text)
 
 
 def _device_call(dev, fn, *args):
@@ -305,7 +302,8 @@ def _policy_rows(logits, action, avail, temperature: float):
 def marl_policy_logprob(logits, action, avail=None, temperature: float = 1.0, top: int = 0) -> dict:
     """Log probability of the action taken, entropy and the `top` best alternatives of each row of logits [..., A] (the q of a
     sampled batch).  action int32 [...], avail uint8 or bool [..., A].  Returns logp, entropy float32 [...], stats float32
-    [..., 2] (for the gradient), top_index int32 and top_logp float32 [..., top] (None with top = 0)."""
+    [..., 2] (for the gradient), top_index int32 and top_logp float32 [..., top] (None with top = 0).  Not recorded by autograd: the
+    gradient is marl_policy_logprob_backward."""
     lead, dev, p = _policy_rows(logits, action, avail, temperature)
     if not 0 <= top <= MAX_TOP:
         raise MarlError(f"top must be in [0, {MAX_TOP}]")
@@ -376,7 +374,7 @@ def _scan_work(s, dev):
 def marl_linear_scan(gate, x, h0=None, done=None, length=None, form: str = "blend", reverse: bool = False, keep: bool = False) -> dict:
     """The gated linear recurrence of x [B, L, C] (its rows and those of gate may be strided; gate may be expanded).  h0 float32 [B, C],
     done uint8 or bool [B, L], length int32 [B], each may be None.  Returns y like x (dense), last float32 [B, C] and, with
-    keep, the states that marl_linear_scan_backward takes."""
+    keep, the states that marl_linear_scan_backward takes.  Not recorded by autograd."""
     s = _scan_args(gate, x, h0, done, length, form, reverse)
     dev = x.device
     B, L, Cn = x.shape
@@ -410,7 +408,7 @@ def marl_linear_scan_backward(gate, x, states, dy, dlast=None, h0=None, done=Non
 def marl_orthogonalise(mats, steps: int = 5, coeffs=(3.4445, -4.7750, 2.0315), eps: float = 1e-7, scale=1.0, out=None) -> list:
     """Orthogonalised updates of a list of matrices [r, c] or batches of them [k, r, c] (one dtype; rows may be strided), in one
     call.  scale: one factor, or one for each entry of the list.  out: a list of tensors like mats (the same ones: in place).
-    Returns the list of results."""
+    Returns the list of results, which autograd does not record."""
     mats = list(mats)
     if not mats:
         return []
